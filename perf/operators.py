@@ -1,0 +1,497 @@
+"""The attention half of a decoder block around the quantized linears, as measurable cases.
+
+In front of every A4 linear stands an RMS norm of the residual stream, which hands the linear its codes (rmsnorm_quantize) and in
+training gives its gradient (rmsnorm_backward).  Behind the qkv projection the new keys and values go into a paged low-bit cache
+(kv_pages_append, kv_pages_read: 3-bit codes, 4 bits for a sequence's first token), and the queries attend over it
+(kv_pages_attention): single tokens, chunks, mixed batches, with or without a sliding window.
+
+A page holds 128 tokens: per key / value head the key codes, the value codes, 128 key scales, 128 value scales, and the lowest
+magnitude bits of a first token.  Codes come 32 to three 32-bit words A, B, C: code i (0 .. 31) has its two magnitude bits in word
+i / 16 at bit 4 (i % 8) + 2 ((i / 8) % 2), and its sign in C at bit 4 (i % 8) + 3 - i / 8.  Keys: [token][channel / 32], code i =
+channel 32 u + i.  Values: [channel][g = 0 .. 3], code i = token 16 (i / 4) + 4 g + i % 4.  Channels are padded to 32.
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+BF16, F32, F64, I32 = torch.bfloat16, torch.float32, torch.float64, torch.int32
+PAGE = 128
+EPS = 1e-5
+NORM_EPS = 1e-5
+SQRT7 = 2.6457512378692627      # float32(sqrt(7))
+TYPES = {"bf16": BF16, "f32": F32}
+
+
+# ---------------------------------------------------------------- the cases
+def _norm(tokens, k, out, dtype="bf16", residual=True):
+    return {"kind": "norm", "tokens": tokens, "k": k, "out": out, "dtype": dtype, "residual": residual}
+
+
+def _grad(tokens, k, dtype="bf16", residual=True):
+    return {"kind": "norm_grad", "tokens": tokens, "k": k, "dtype": dtype, "residual": residual}
+
+
+def _cache(seqs, new, ctx, heads, dim, ragged=False):
+    return {"kind": "cache", "seqs": seqs, "new": new, "ctx": ctx, "heads": heads, "dim": dim, "ragged": ragged}
+
+
+def _attn(seqs, new, ctx, q_heads, kv_heads, dim, window=0, sinks=0, q_bits=16, mix="same"):
+    """mix: "same" (every sequence alike), "ragged" (lengths spread), "mixed" (one chunk among single tokens)."""
+    return {"kind": "attn", "seqs": seqs, "new": new, "ctx": ctx, "q_heads": q_heads, "kv_heads": kv_heads, "dim": dim,
+            "window": window, "sinks": sinks, "q_bits": q_bits, "mix": mix}
+
+
+def listed():
+    return [
+        # one sequence decoding: the norm before a 7B layer's qkv projection; launch and latency are all there is
+        dict(_norm(1, 4096, "int4"), name="norm_int4_1"),
+        # an evaluation batch before a dense INT8 linear, FFN width no multiple of 8
+        dict(_norm(2000, 5460, "int8"), name="norm_int8_2000"),
+        # four prompts of 4096 tokens: codes for the block-float product
+        dict(_norm(16384, 4096, "int4_mx"), name="norm_int4_mx_16384"),
+        # a training step of a 3B layer: the norm's gradient, joined by the residual stream's
+        dict(_grad(4096, 3200), name="norm_grad_4096"),
+        # a small float32 run, rows of an odd length
+        dict(_grad(777, 1537, "f32", False), name="norm_grad_f32_777"),
+        # a serving batch, each sequence one token on
+        dict(_cache(32, 1, 4096, 8, 128, True), name="cache_decode_32"),
+        # a prompt of 4096 tokens with all its heads
+        dict(_cache(1, 4096, 0, 32, 128), name="cache_prompt_4096"),
+        # one sequence decoding, a key / value head to each query head
+        dict(_attn(1, 1, 4096, 32, 32, 128), name="attn_decode_1"),
+        # a full serving batch of ragged lengths, four query heads to a key / value head
+        dict(_attn(64, 1, 8192, 32, 8, 128, mix="ragged"), name="attn_decode_64"),
+        # one very long sequence, where the work has to be split over its keys
+        dict(_attn(1, 1, 131071, 32, 8, 128), name="attn_decode_long"),
+        # a chunk of a chunked prefill: 2048 new tokens behind 6144 cached ones
+        dict(_attn(1, 2048, 6144, 32, 8, 128), name="attn_chunk_2048"),
+        # a chunk among decoding sequences, 4-bit queries, a sliding window with sinks, heads of 64 channels
+        dict(_attn(16, 500, 4000, 32, 32, 64, 1024, 4, 4, "mixed"), name="attn_window_mixed"),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    kind = rng.choice(["norm", "norm", "norm_grad", "cache", "attn", "attn", "attn", "attn"])
+    if kind == "norm":
+        return _norm(_log_int(rng, 1, 16384), _log_int(rng, 256, 4096), rng.choice(["int4", "int4_mx", "int8"]),
+                     rng.choice(["bf16", "bf16", "f32"]), rng.random() < 0.7)
+    if kind == "norm_grad":
+        return _grad(_log_int(rng, 16, 4096), _log_int(rng, 256, 4096), rng.choice(["bf16", "bf16", "f32"]), rng.random() < 0.7)
+    dim = rng.choice([64, 64, 96, 100, 128, 128, 128, 256])
+    if kind == "cache":
+        if rng.random() < 0.5:
+            return _cache(_log_int(rng, 1, 64), rng.randint(1, 3), _log_int(rng, 1, 4096), rng.randint(1, 16), dim, True)
+        return _cache(rng.randint(1, 4), _log_int(rng, 16, 1024), _log_int(rng, 1, 2048), rng.randint(1, 16), dim, True)
+    kv = rng.choice([1, 2, 4, 5, 8])
+    group = rng.choice([g for g in (1, 2, 3, 4, 5, 8) if kv * g * dim <= 4096])
+    window = 0 if rng.random() < 0.6 else _log_int(rng, 16, 2048)
+    sinks = rng.choice([0, 1, 4, 130]) if window else 0
+    q_bits = rng.choice([16, 16, 4])
+    if rng.random() < 0.5:      # decode
+        seqs = _log_int(rng, 1, 64)
+        return _attn(seqs, rng.choice([1, 1, 1, 4]), _log_int(rng, 1, 65536 // seqs), kv * group, kv, dim, window, sinks, q_bits,
+                     rng.choice(["same", "ragged"]))
+    seqs = rng.randint(1, 8)
+    return _attn(seqs, _log_int(rng, 16, 1500 // seqs), _log_int(rng, 1, 4096), kv * group, kv, dim, window, sinks, q_bits,
+                 rng.choice(["same", "ragged", "mixed"]))
+
+
+def _lengths(case):
+    """(new tokens, cached tokens before them) of every sequence: a matter of the case, not of the seed."""
+    rng = random.Random("%s" % sorted((k, v) for k, v in case.items() if k != "name"))
+    s, new, ctx = case["seqs"], case["new"], case["ctx"]
+    mix = case.get("mix", "ragged" if case.get("ragged") else "same")
+    if mix == "same":
+        return [new] * s, [ctx] * s
+    if mix == "mixed":
+        n = [1] * s
+        n[rng.randrange(s)] = new
+        return n, [rng.randint(0, ctx) for _ in range(s)]
+    return [new if new < 8 else rng.randint(1, new) for _ in range(s)], [rng.randint(0, ctx) for _ in range(s)]
+
+
+# ---------------------------------------------------------------- inputs
+def _heavy(g, m, k, dtype):
+    """N(0, 1) with about 0.5 % of the channels ten times as large, as residual streams have them."""
+    x = torch.randn((m, k), generator=g, device="cuda", dtype=F32)
+    ch = torch.randperm(k, generator=g, device="cuda")[:max(1, round(0.005 * k))]
+    x[:, ch] *= 10.0
+    return x.to(dtype)
+
+
+def _rope_table(n, dim):
+    """[positions, dim] float32: cosines of position * 10000^(-2 i / dim), i < dim / 2, then the sines."""
+    inv = 10000.0 ** (-2.0 * torch.arange(dim // 2, device="cuda", dtype=F64) / dim)
+    a = torch.arange(n, device="cuda", dtype=F64)[:, None] * inv
+    return torch.cat([a.cos(), a.sin()], 1).to(F32)
+
+
+def _page_bytes(heads, dim):
+    units = (dim + 31) // 32
+    return heads * (2 * PAGE * units * 12 + 2 * PAGE * 4 + 128)
+
+
+def _pack(mag, sign):
+    """Magnitudes 0 .. 3 and signs, int32 [..., 32] -> words [..., 3]."""
+    w = [torch.zeros(mag.shape[:-1], dtype=I32, device=mag.device) for _ in range(3)]
+    for i in range(32):
+        w[i // 16] |= mag[..., i] << (4 * (i % 8) + 2 * ((i // 8) % 2))
+        w[2] |= sign[..., i] << (4 * (i % 8) + 3 - i // 8)
+    return torch.stack(w, -1)
+
+
+def _filled_pages(g, n_pages, heads, dim, first):
+    """Pages of quantized Gaussian heads; the pages `first` (int64) begin a sequence."""
+    units, dev = (dim + 31) // 32, "cuda"
+    raw = torch.zeros((n_pages, heads, _page_bytes(1, dim)), dtype=torch.uint8, device=dev)
+    words = raw.view(I32)
+    nw = PAGE * units * 3
+    is_first = torch.zeros(n_pages, dtype=torch.bool, device=dev)
+    is_first[first] = True
+    step = max(1, (1 << 26) // (PAGE * heads * dim))
+    for lo in range(0, n_pages, step):
+        n = min(step, n_pages - lo)
+        for part in range(2):
+            x = torch.randn((n, heads, PAGE, dim), generator=g, device=dev, dtype=F32)
+            if part == 0:       # some key channels are larger than the others
+                x *= 1.0 + 2.0 * (torch.rand((heads, 1, dim), generator=g, device=dev) < 0.05)
+            gamma = x.abs().amax(-1, keepdim=True)
+            qb = torch.full((n, 1, PAGE, 1), 3.0, device=dev)
+            qb[is_first[lo:lo + n], :, 0] = 7.0
+            q = torch.round(x * (qb / (gamma + EPS)))
+            x = torch.zeros((n, heads, PAGE, 32 * units), dtype=I32, device=dev)
+            x[..., :dim] = q.to(I32)
+            mag, sign = x.abs(), (x < 0).to(I32)
+            f = is_first[lo:lo + n].nonzero()[:, 0]
+            low = mag[f, :, 0] & 1                                          # [first pages, heads, channels]
+            mag[f, :, 0] = mag[f, :, 0] >> 1
+            at = words[lo:lo + n]
+            if part == 0:
+                at[:, :, :nw] = _pack(mag.view(n, heads, PAGE, units, 32), sign.view(n, heads, PAGE, units, 32)).reshape(n, heads, nw)
+            else:
+                by = [t.view(n, heads, 8, 4, 4, 32 * units).permute(0, 1, 5, 3, 2, 4).reshape(n, heads, 32 * units, 4, 32)
+                      for t in (mag, sign)]                                 # [t, g, r, channel] -> [channel, g, (t, r)]
+                at[:, :, nw:2 * nw] = _pack(*by).reshape(n, heads, nw)
+            at.view(F32)[:, :, 2 * nw + PAGE * part:2 * nw + PAGE * (part + 1)] = (gamma / qb)[..., 0]
+            i = torch.arange(32, device=dev)
+            bits = low.view(-1, heads, units, 32) << (4 * (i % 8) + 3 - i // 8).to(I32)
+            at[f, :, 2 * nw + 2 * PAGE + units * part:2 * nw + 2 * PAGE + units * (part + 1)] = bits.sum(-1).to(I32)
+    return raw.view(n_pages, heads * _page_bytes(1, dim))
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(7001 + seed)
+    dev, kind = "cuda", case["kind"]
+    if kind in ("norm", "norm_grad"):
+        m, k, dt = case["tokens"], case["k"], TYPES[case["dtype"]]
+        gamma = 1.0 + 0.2 * torch.randn(k, generator=g, device=dev, dtype=F32)
+        x = _heavy(g, m, k, dt)
+        r = _heavy(g, m, k, dt) if case["residual"] else None
+        if kind == "norm":
+            return {"case": case, "x": x, "r": r, "gamma": gamma}
+        rstd = torch.rsqrt(x.double().square().mean(-1) + NORM_EPS).to(F32)
+        dy = (1e-3 * torch.randn((m, k), generator=g, device=dev, dtype=F32)).to(dt)
+        return {"case": case, "h": x, "rstd": rstd, "gamma": gamma, "dy": dy, "dh": None if r is None else (1e-3 * r).to(dt)}
+
+    new, ctx = _lengths(case)
+    s, dim = case["seqs"], case["dim"]
+    heads = case["heads"] if kind == "cache" else case["kv_heads"]
+    total = [n + c for n, c in zip(new, ctx)]
+    counts = [(t + PAGE - 1) // PAGE for t in total]
+    max_pages, n_pages = max(counts), sum(counts) + 3
+    # pages of the pool in any order, a table row's unused places -1
+    ids = torch.randperm(n_pages, generator=g, device=dev)[:sum(counts)].to(I32)
+    table = torch.full((s, max_pages), -1, dtype=I32, device=dev)
+    used = torch.arange(max_pages, device=dev)[None] < torch.tensor(counts, device=dev)[:, None]
+    table[used] = ids
+    st = {"case": case, "table": table, "rope": _rope_table(max_pages * PAGE, dim),
+          "q_start": torch.tensor([sum(new[:i]) for i in range(s + 1)], dtype=I32, device=dev),
+          "kv_len": torch.tensor(total, dtype=I32, device=dev), "max_new": max(new), "heads": heads}
+    t = sum(new)
+    if kind == "cache":
+        st["pages"] = torch.zeros((n_pages, _page_bytes(heads, dim)), dtype=torch.uint8, device=dev)
+        qkv = torch.randn((t, 3 * heads * dim), generator=g, device=dev, dtype=F32).to(BF16)   # as the qkv product leaves it
+        st["k"], st["v"] = (qkv[:, i * heads * dim:(i + 1) * heads * dim].view(t, heads, dim) for i in (1, 2))
+        return st
+    hq = case["q_heads"]
+    st["pages"] = _filled_pages(g, n_pages, heads, dim, table[:, 0].long())
+    qkv = (2.0 * torch.randn((t, (hq + 2 * heads) * dim), generator=g, device=dev, dtype=F32)).to(BF16)
+    st["q"] = qkv[:, :hq * dim].view(t, hq, dim)
+    return st
+
+
+# ---------------------------------------------------------------- one pass
+def _quantized(y, out):
+    """Values of the codes of float32 rows: INT4 absmean or INT8 absmax."""
+    k = y.shape[-1]
+    if out == "int8":
+        top = y.abs().amax(-1, keepdim=True)
+        q = torch.round(y * (127.0 / (top + EPS))).clamp_(-128, 127)
+        scale = top / 127.0
+    else:
+        beta = (y.double().abs().sum(-1, keepdim=True) / k).to(F32)
+        root = torch.full_like(beta, SQRT7)
+        q = torch.round(y * (root / (beta + EPS))).clamp_(-8, 7)
+        scale = beta / root
+    return (q * scale).to(BF16), scale[:, 0]
+
+
+def _positions(st):
+    """Sequence and position of every new token."""
+    qs = st["q_start"].long()
+    n = qs[1:] - qs[:-1]
+    t = int(st["k" if "k" in st else "q"].shape[0])
+    seq = torch.repeat_interleave(torch.arange(n.numel(), device=qs.device), n, output_size=t)
+    return seq, st["kv_len"].long()[seq] - n[seq] + torch.arange(t, device=qs.device) - qs[seq]
+
+
+def _rotate(x, rope, pos):
+    """float32 [T, H, D]: channels i and i + D / 2 as a pair."""
+    half = x.shape[-1] // 2
+    c, s = rope[pos, None, :half], rope[pos, None, half:]
+    a, b = x[..., :half], x[..., half:]
+    return torch.cat([a * c - b * s, b * c + a * s], -1)
+
+
+def _head_values(x, qb):
+    gamma = x.abs().amax(-1, keepdim=True)
+    q = torch.maximum(torch.minimum(torch.round(x * (qb / (gamma + EPS))), qb), -qb)
+    return q, gamma / qb
+
+
+def _codes(words):
+    """Words [..., 3] -> codes [..., 32], signed, of the two stored magnitude bits."""
+    i = torch.arange(32, device=words.device)
+    mag = (words[..., i // 16] >> (4 * (i % 8) + 2 * ((i // 8) % 2)).to(I32)) & 3
+    neg = (words[..., 2:] >> (4 * (i % 8) + 3 - i // 8).to(I32)) & 1
+    return mag, 1 - 2 * neg
+
+
+def _cached(st, dim):
+    """Keys and values of every table place, float32 [S, heads, places, D]; places without a page are zero."""
+    table, heads, units = st["table"].long(), st["heads"], (dim + 31) // 32
+    s, mp = table.shape
+    words = st["pages"].view(I32).view(-1, heads, _page_bytes(1, dim) // 4)[table.clamp_min(0)]
+    nw = PAGE * units * 3
+    i = torch.arange(32, device=words.device)
+    out = []
+    for part in range(2):
+        mag, sign = _codes(words[..., part * nw:(part + 1) * nw].reshape(s, mp, heads, -1, 3))
+        low = words[:, 0, :, 2 * nw + 2 * PAGE + part * units:2 * nw + 2 * PAGE + (part + 1) * units]
+        low = ((low[..., None] >> (4 * (i % 8) + 3 - i // 8).to(I32)) & 1).reshape(s, heads, 32 * units)
+        if part == 0:
+            mag, sign = (t.reshape(s, mp, heads, PAGE, 32 * units) for t in (mag, sign))
+        else:
+            mag, sign = (t.reshape(s, mp, heads, 32 * units, 4, 8, 4).permute(0, 1, 2, 5, 4, 6, 3).reshape(s, mp, heads, PAGE, 32 * units)
+                         for t in (mag, sign))
+        mag = mag.clone()
+        mag[:, 0, :, 0] = 2 * mag[:, 0, :, 0] + low
+        scale = words.view(F32)[..., 2 * nw + part * PAGE:2 * nw + (part + 1) * PAGE]
+        val = (mag * sign).to(F32) * scale[..., None]
+        val = torch.where((table >= 0)[:, :, None, None, None], val, torch.zeros((), device=val.device))
+        out.append(val.permute(0, 2, 1, 3, 4).reshape(s, heads, mp * PAGE, 32 * units)[..., :dim])
+    return out
+
+
+def _plain_attention(st):
+    case = st["case"]
+    hq, hk, d, s = case["q_heads"], case["kv_heads"], case["dim"], case["seqs"]
+    seq, pos = _positions(st)
+    q = _rotate(st["q"].float(), st["rope"], pos)
+    if case["q_bits"] == 4:
+        code, scale = _head_values(q, torch.full_like(q[..., :1], 7.0))
+        q = code * scale
+    k, v = _cached(st, d)
+    n, places, dev = st["max_new"], k.shape[2], q.device
+    row = torch.arange(q.shape[0], device=dev) - st["q_start"].long()[seq]
+    padded = torch.zeros((s, n, hq, d), device=dev)
+    padded[seq, row] = q
+    at = torch.full((s, n), -1, dtype=torch.int64, device=dev)
+    at[seq, row] = pos
+    qg = padded.view(s, n, hk, hq // hk, d).permute(0, 2, 3, 1, 4).reshape(s * hk, -1, d)
+    logits = torch.bmm(qg, k.reshape(s * hk, places, d).transpose(1, 2).contiguous())
+    logits = logits.view(s, hk, hq // hk, n, places).mul_(d ** -0.5)
+    j, i = torch.arange(places, device=dev), at[:, None, None, :, None]
+    seen = j <= i
+    if case["window"]:
+        seen = seen & ((j > i - case["window"]) | (j < case["sinks"]))
+    logits.masked_fill_(~seen, float("-inf"))
+    top = logits.amax(-1, keepdim=True).clamp_min(-3e38)
+    p = logits.sub_(top).exp_()
+    o = torch.bmm(p.view(s * hk, -1, places), v.reshape(s * hk, places, d).contiguous()).view(s, hk, hq // hk, n, d)
+    o = o / p.sum(-1, keepdim=True).clamp_min(1e-30)
+    return o.permute(0, 3, 1, 2, 4).reshape(s, n, hq, d)[seq, row].to(BF16)
+
+
+def run(st):
+    case = st["case"]
+    kind = case["kind"]
+    if own:
+        from paper_2411_04965_amd import binding as B
+        if kind == "norm":
+            mode = {"int4": B.BL_ACT_INT4_ABSMEAN, "int4_mx": B.BL_ACT_INT4_ABSMEAN_MX6, "int8": B.BL_ACT_TOPK_INT8_ABSMAX}[case["out"]]
+            r = B.rmsnorm_quantize(st["x"], st["gamma"], mode, residual=st["r"], norm_eps=NORM_EPS, eps=EPS)
+            codes = B.unpack_act(r["q"], mode, case["tokens"], case["k"])
+            values = torch.empty(codes.shape, dtype=BF16, device=codes.device)
+            torch.mul(codes, r["scale"][:, None], out=values)
+            return {"values": values, "scale": r["scale"], "rstd": r["rstd"], "h": r["h"]}
+        if kind == "norm_grad":
+            dx, dgamma = B.rmsnorm_backward(st["dy"], st["h"], st["rstd"], st["gamma"], dH=st["dh"])
+            return {"dx": dx, "dgamma": dgamma}
+        if kind == "cache":
+            B.kv_pages_append(st["k"], st["v"], st["pages"], st["table"], st["q_start"], st["kv_len"], rope=st["rope"], eps=EPS)
+            k, v = B.kv_pages_read(st["pages"], st["table"], st["q_start"], st["kv_len"], st["k"].shape[0], case["heads"],
+                                   case["dim"], out_dtype=BF16)
+            return {"k": k, "v": v}
+        return {"o": B.kv_pages_attention(st["q"], st["pages"], st["table"], st["q_start"], st["kv_len"], case["kv_heads"],
+                                          rope=st["rope"], window=case["window"], sinks=case["sinks"], q_bits=case["q_bits"],
+                                          eps=EPS)}
+    if kind == "norm":
+        h = st["x"] if st["r"] is None else (st["x"].float() + st["r"].float()).to(st["x"].dtype)
+        rstd = (1.0 / (h.double().square().mean(-1) + NORM_EPS).sqrt()).to(F32)
+        values, scale = _quantized((h.float() * rstd[:, None]) * st["gamma"], case["out"])
+        return {"values": values, "scale": scale, "rstd": rstd, "h": h}
+    if kind == "norm_grad":
+        dy, xh = st["dy"].float(), st["h"].float() * st["rstd"][:, None]
+        a = dy * st["gamma"]
+        dx = st["rstd"][:, None] * (a - xh * (a * xh).mean(-1, keepdim=True))
+        if st["dh"] is not None:
+            dx = dx + st["dh"].float()
+        return {"dx": dx.to(st["h"].dtype), "dgamma": (dy * xh).sum(0, dtype=F64).to(F32)}
+    if kind == "cache":
+        _, pos = _positions(st)
+        qb = torch.where(pos == 0, 7.0, 3.0)[:, None, None]
+        out = {}
+        for name, x in (("k", _rotate(st["k"].float(), st["rope"], pos)), ("v", st["v"].float())):
+            code, scale = _head_values(x, qb)
+            out[name] = (code * scale).to(BF16)
+        return out
+    return {"o": _plain_attention(st)}
+
+
+# ---------------------------------------------------------------- what a pass cannot do without
+def _visible(n, ctx, window, sinks):
+    """(query, key) pairs, and keys that some query sees, of one sequence."""
+    pairs, lo = 0, ctx
+    for p in range(ctx, ctx + n):
+        first = max(0, p - window + 1) if window else 0
+        pairs += p + 1 - first + min(sinks, first)
+        lo = min(lo, first)
+    return pairs, ctx + n - lo + min(sinks, lo)
+
+
+def work(case):
+    if case["kind"] in ("norm", "norm_grad"):
+        m, k, e = case["tokens"], case["k"], 2 if case["dtype"] == "bf16" else 4
+        if case["kind"] == "norm":      # x and r in, h (where it is new) and the codes' values out
+            return {"bytes": m * k * (e * (3 if case["residual"] else 1) + 2) + 8 * m + 4 * k, "flops": 10 * m * k}
+        return {"bytes": m * k * e * (4 if case["residual"] else 3) + 4 * m + 8 * k, "flops": 10 * m * k}
+    new, ctx = _lengths(case)
+    d, t = case["dim"], sum(new)
+    if case["kind"] == "cache":         # states in, codes and scales out, values out
+        return {"bytes": 2 * t * case["heads"] * (2 * d + 3 * d / 8 + 4 + 2 * d) + 4 * t * d, "flops": 10 * t * case["heads"] * d}
+    both = [_visible(n, c, case["window"], case["sinks"]) for n, c in zip(new, ctx)]
+    cached = sum(b[1] for b in both) * case["kv_heads"] * 2 * (3 * d / 8 + 4)
+    return {"bytes": cached + 4 * t * case["q_heads"] * d + 4 * t * d, "flops": 4 * sum(b[0] for b in both) * case["q_heads"] * d}
+
+
+# ---------------------------------------------------------------- the definition in 64 bits
+def exact(case, seed):
+    st = prepare(case, seed)
+    kind = case["kind"]
+    if kind == "norm":
+        h = st["x"].double()
+        if st["r"] is not None:
+            h = (h + st["r"].double()).to(st["x"].dtype).double()           # the stream is kept in its own type
+        rstd = (h.pow(2).sum(1) / case["k"] + NORM_EPS).pow(-0.5)
+        y = h * rstd[:, None] * st["gamma"].double()
+        if case["out"] == "int8":
+            unit = y.abs().max(1).values
+            step, lo, hi, stat = unit / 127, -128, 127, 127 / (unit + EPS)
+        else:
+            unit = y.abs().mean(1)
+            step, lo, hi, stat = unit / 7 ** 0.5, -8, 7, 7 ** 0.5 / (unit + EPS)
+        return {"values": (y * stat[:, None]).round().clamp(lo, hi) * step[:, None], "scale": step, "rstd": rstd, "h": h}
+    if kind == "norm_grad":
+        # d/dh of sum(dy * gamma * h * rstd(h)) in the quotient form, with the given rstd as the value of 1 / |h|
+        dy, h, rs, ga = (st[n].double() for n in ("dy", "h", "rstd", "gamma"))
+        dot = (dy * ga * h).sum(1)
+        dx = rs[:, None] * dy * ga - h * (dot * rs.pow(3) / case["k"])[:, None]
+        if st["dh"] is not None:
+            dx += st["dh"].double()
+        return {"dx": dx, "dgamma": torch.mv((dy * h).t(), rs)}
+
+    qs, ln, dim = st["q_start"].tolist(), st["kv_len"].tolist(), case["dim"]
+    half = dim // 2
+    turn = torch.complex(st["rope"][:, :half].double(), st["rope"][:, half:].double())
+    spin = lambda x, p: torch.view_as_real(torch.complex(x[..., :half], x[..., half:]) * turn[p][:, None]).permute(0, 1, 3, 2).flatten(2)  # noqa: E731
+
+    def grid(x, top):
+        unit = x.abs().max(-1, keepdim=True).values
+        return (x * (top / (unit + EPS))).round().clamp(-top, top) * unit / top
+
+    if kind == "cache":
+        out = {"k": [], "v": []}
+        for s in range(case["seqs"]):
+            n = qs[s + 1] - qs[s]
+            p = torch.arange(ln[s] - n, ln[s], device="cuda")
+            for name in out:
+                x = st[name][qs[s]:qs[s + 1]].double()
+                x = spin(x, p) if name == "k" else x
+                y = grid(x, 3)
+                if ln[s] == n:
+                    y[0] = grid(x[0], 7)
+                out[name].append(y)
+        return {name: torch.cat(v) for name, v in out.items()}
+
+    hq, hk, units = case["q_heads"], case["kv_heads"], (dim + 31) // 32
+    words = st["pages"].view(I32).view(-1, hk, _page_bytes(1, dim) // 4)
+    nw = PAGE * units * 3
+
+    def value(w, i):
+        m = (w[..., i // 16] >> (4 * (i % 8) + 2 * (i // 8 % 2))) & 3
+        return torch.where((w[..., 2] >> (4 * (i % 8) + 3 - i // 8)) & 1 == 1, -m, m).double()
+
+    o = torch.empty((qs[-1], hq, dim), dtype=F64, device="cuda")
+    for s in range(case["seqs"]):
+        n, length = qs[s + 1] - qs[s], ln[s]
+        mine = words[st["table"][s, :(length + PAGE - 1) // PAGE].long()]
+        p = torch.arange(length - n, length, device="cuda")
+        q = spin(st["q"][qs[s]:qs[s + 1]].double(), p)
+        q = grid(q, 7) if case["q_bits"] == 4 else q
+        j = torch.arange(length, device="cuda")
+        seen = j[None] <= p[:, None]
+        if case["window"]:
+            seen &= (p[:, None] - j[None] < case["window"]) | (j[None] < case["sinks"])
+        for h in range(hk):
+            kw = mine[:, h, :nw].reshape(-1, units, 3)                          # [tokens, unit]
+            vw = mine[:, h, nw:2 * nw].reshape(-1, 32 * units, 4, 3)            # [pages, channel, g]
+            k = torch.stack([value(kw, i) for i in range(32)], -1).flatten(1)
+            v = torch.empty((mine.shape[0], PAGE, 32 * units), dtype=F64, device="cuda")
+            for i in range(32):
+                for g in range(4):
+                    v[:, 16 * (i // 4) + 4 * g + i % 4] = value(vw[:, :, g], i)
+            v = v.flatten(0, 1)
+            head = mine[0, h].cpu()                                          # the first token has one bit more
+            lows, kw, vw = head[2 * nw + 2 * PAGE:].tolist(), head[:nw].view(-1, units, 3)[0, :, 2].tolist(), head[nw:2 * nw].view(-1, 4, 3)[:, 0, 2].tolist()
+            more = [[], []]
+            for c in range(32 * units):
+                at = 4 * (c % 8) + 3 - c % 32 // 8
+                more[0].append((lows[c // 32] >> at & 1) * (1 - 2 * (kw[c // 32] >> at & 1)))
+                more[1].append((lows[units + c // 32] >> at & 1) * (1 - 2 * (vw[c] >> 3 & 1)))
+            for part, x in enumerate((k, v)):
+                x[0] = 2 * x[0] + torch.tensor(more[part], dtype=F64, device="cuda")
+                x *= mine[:, h, 2 * nw + part * PAGE:2 * nw + (part + 1) * PAGE].contiguous().view(F32).double().reshape(-1, 1)
+            k, v = k[:length, :dim], v[:length, :dim]
+            for a in range(h * hq // hk, (h + 1) * hq // hk):
+                z = (q[:, a] @ k.t()) / dim ** 0.5
+                o[qs[s]:qs[s + 1], a] = torch.softmax(z.masked_fill(~seen, float("-inf")), -1) @ v
+    return {"o": o}
