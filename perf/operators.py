@@ -7,8 +7,9 @@ training gives its gradient (rmsnorm_backward).  Behind the qkv projection the n
 
 A page holds 128 tokens: per key / value head the key codes, the value codes, 128 key scales, 128 value scales, and the lowest
 magnitude bits of a first token.  Codes come 32 to three 32-bit words A, B, C: code i (0 .. 31) has its two magnitude bits in word
-i / 16 at bit 4 (i % 8) + 2 ((i / 8) % 2), and its sign in C at bit 4 (i % 8) + 3 - i / 8.  Keys: [token][channel / 32], code i =
-channel 32 u + i.  Values: [channel][g = 0 .. 3], code i = token 16 (i / 4) + 4 g + i % 4.  Channels are padded to 32.
+i / 16 at bit 4 (i % 8) + 2 ((i / 8) % 2), and its sign in C at bit 4 (i % 8) + 3 - i / 8.  Keys: [slot][channel / 32], code i =
+channel i of the 32, where token 64 a + 16 b + 4 c + d has slot 64 a + 16 c + 4 b + d.  Values: [channel][token / 32], code i = token i
+of the 32.  Channels are padded to 32.
 """
 import math
 import random
@@ -174,10 +175,10 @@ def _filled_pages(g, n_pages, heads, dim, first):
             mag[f, :, 0] = mag[f, :, 0] >> 1
             at = words[lo:lo + n]
             if part == 0:
-                at[:, :, :nw] = _pack(mag.view(n, heads, PAGE, units, 32), sign.view(n, heads, PAGE, units, 32)).reshape(n, heads, nw)
+                by = [t.view(n, heads, 2, 4, 4, 4, units, 32).transpose(3, 4) for t in (mag, sign)]         # tokens to slots
+                at[:, :, :nw] = _pack(*by).reshape(n, heads, nw)
             else:
-                by = [t.view(n, heads, 8, 4, 4, 32 * units).permute(0, 1, 5, 3, 2, 4).reshape(n, heads, 32 * units, 4, 32)
-                      for t in (mag, sign)]                                 # [t, g, r, channel] -> [channel, g, (t, r)]
+                by = [t.view(n, heads, 4, 32, 32 * units).permute(0, 1, 4, 2, 3) for t in (mag, sign)]
                 at[:, :, nw:2 * nw] = _pack(*by).reshape(n, heads, nw)
             at.view(F32)[:, :, 2 * nw + PAGE * part:2 * nw + PAGE * (part + 1)] = (gamma / qb)[..., 0]
             i = torch.arange(32, device=dev)
@@ -288,10 +289,10 @@ def _cached(st, dim):
         low = words[:, 0, :, 2 * nw + 2 * PAGE + part * units:2 * nw + 2 * PAGE + (part + 1) * units]
         low = ((low[..., None] >> (4 * (i % 8) + 3 - i // 8).to(I32)) & 1).reshape(s, heads, 32 * units)
         if part == 0:
-            mag, sign = (t.reshape(s, mp, heads, PAGE, 32 * units) for t in (mag, sign))
-        else:
-            mag, sign = (t.reshape(s, mp, heads, 32 * units, 4, 8, 4).permute(0, 1, 2, 5, 4, 6, 3).reshape(s, mp, heads, PAGE, 32 * units)
+            mag, sign = (t.reshape(s, mp, heads, 2, 4, 4, 4, 32 * units).transpose(4, 5).reshape(s, mp, heads, PAGE, 32 * units)
                          for t in (mag, sign))
+        else:
+            mag, sign = (t.reshape(s, mp, heads, 32 * units, PAGE).transpose(3, 4) for t in (mag, sign))
         mag = mag.clone()
         mag[:, 0, :, 0] = 2 * mag[:, 0, :, 0] + low
         scale = words.view(F32)[..., 2 * nw + part * PAGE:2 * nw + (part + 1) * PAGE]
@@ -472,13 +473,14 @@ def exact(case, seed):
         if case["window"]:
             seen &= (p[:, None] - j[None] < case["window"]) | (j[None] < case["sinks"])
         for h in range(hk):
-            kw = mine[:, h, :nw].reshape(-1, units, 3)                          # [tokens, unit]
-            vw = mine[:, h, nw:2 * nw].reshape(-1, 32 * units, 4, 3)            # [pages, channel, g]
+            slot = [64 * (t // 64) + 16 * (t % 16 // 4) + 4 * (t % 64 // 16) + t % 4 for t in range(PAGE)]
+            kw = mine[:, h, :nw].reshape(-1, PAGE, units, 3)[:, slot].flatten(0, 1)         # [tokens, unit]
+            vw = mine[:, h, nw:2 * nw].reshape(-1, 32 * units, 4, 3)            # [pages, channel, token / 32]
             k = torch.stack([value(kw, i) for i in range(32)], -1).flatten(1)
             v = torch.empty((mine.shape[0], PAGE, 32 * units), dtype=F64, device="cuda")
             for i in range(32):
                 for g in range(4):
-                    v[:, 16 * (i // 4) + 4 * g + i % 4] = value(vw[:, :, g], i)
+                    v[:, 32 * g + i] = value(vw[:, :, g], i)
             v = v.flatten(0, 1)
             head = mine[0, h].cpu()                                          # the first token has one bit more
             lows, kw, vw = head[2 * nw + 2 * PAGE:].tolist(), head[:nw].view(-1, units, 3)[0, :, 2].tolist(), head[nw:2 * nw].view(-1, 4, 3)[:, 0, 2].tolist()
