@@ -350,6 +350,82 @@ int kv_cache_append(const void* X, bl_dtype x_dtype, int64_t T, int64_t H, int64
 int kv_cache_read(const void* cache, const float* scales, int64_t pos0, int64_t T, int64_t H, int64_t D,
                   void* out, bl_dtype out_dtype, void* stream);
 
+/* The same cache in pages, for a batch of sequences whose memory is handed out as they grow, and attention over it.  A page holds
+ * BL_KV_PAGE = 128 consecutive positions of one sequence, all heads, keys and values; page k of a sequence its positions 128 k ...
+ * 128 k + 127.  The codes are those of quantize_heads (3 bits, Q_b = 3; at position 0 4 bits, Q_b = 7), each head vector on its own,
+ * as sign and magnitude so that the attention's matrix instructions take them with a few shifts and masks.
+ *   One head of a page is kv_page_bytes(1, D) bytes, heads in order: key codes, value codes, float32 key scales [128], float32 value
+ *   scales [128], low magnitude bits (128 bytes).  With D rounded up to U = ceil(D / 32) groups of 32 channels (padding channels have
+ *   code 0): 32 codes take three 32-bit words A, B, C; code i has its two magnitude bits in A (i < 16) or B at bit 4 (i % 8) +
+ *   2 ((i / 8) % 2) and its sign in C at bit 4 (i % 8) + 3 - i / 8.  Key codes: [slot][U], code i = channel 32 u + i, where token
+ *   64 a + 16 b + 4 c + d of the page (a < 2, the others < 4) has slot 64 a + 16 c + 4 b + d.  Value codes: [channel][4], code i =
+ *   token 32 g + i.  A 4-bit level has |q| / 2 as its magnitude there, and |q| % 2 in the low magnitude bits: U words of keys, then U
+ *   words of values, channel i of the 32 at C's bit; they belong to the page's token 0 and mean something in a sequence's page 0 only.
+ * How a batch is given, to all three calls:
+ *   pages      device, n_pages pages of kv_page_bytes(H, D) bytes, 128-byte aligned (the pool)
+ *   page_table device, int32 [n_seqs, max_pages]: the pool's page that holds page k of sequence s.  An entry outside 0 .. n_pages - 1
+ *              is a page that is not there: its positions are neither written nor read nor attended to.
+ *   q_start    device, int32 [n_seqs + 1], ascending from 0: rows q_start[s] .. q_start[s + 1] - 1 of the T rows are sequence s's
+ *              last ones, in order (none: the sequence has no row in this call)
+ *   kv_len     device, int32 [n_seqs]: length of the sequence with these rows; the last of them is position kv_len[s] - 1.  Rows
+ *              before position 0 and positions from 128 max_pages on are treated as absent.
+ *   The host reads none of these arrays: calls can be captured and replayed with other contents.  Rows of the outputs that belong to
+ *   no sequence are left as they were.  A pool page that a call writes belongs to one sequence; read, it can be shared.
+ *   rope       nullable; device, float32 [n_pos, D], n_pos >= 128 max_pages: per position the cosines for channel pairs (i, i + D / 2),
+ *              i < D / 2, then their sines.  Keys and queries are rotated on the way in: x_i c - x_(i+D/2) s, x_(i+D/2) c + x_i s.
+ *   D          even, 2 ... 256
+ * kv_pages_append: K, V device [T, H, D] of x_dtype, row t at element t * ldk, t * ldv (ldk, ldv >= H * D, heads dense), 16-byte
+ *   aligned bases.  Float32 steps as in quantize_heads; rows are written whatever order sequences and pages stand in.
+ * kv_pages_read: the values of the batch's rows, K_out, V_out [T, H, D] of out_dtype, dense (either may be NULL).  (With q_start the
+ *   running sums of kv_len it reads whole sequences.)
+ * kv_pages_attention: O[t] = sum_j p_j v_j / sum_j p_j over the visible positions j of the row's sequence, p_j = exp(scale * q . k_j)
+ *   relative to the largest; position j is visible to a row at position i if j <= i, and, where window > 0, j > i - window or
+ *   j < sinks.  A row that sees nothing (or only absent pages) gives zeros.
+ *   Q          device [T, Hq, D] of q_dtype, row t at element t * ldq, 16-byte aligned; Hq a multiple of H: query head h reads head
+ *              h / (Hq / H)
+ *   q_bits     16: queries as they are (kept to 8 significand bits, so bfloat16 ones exactly); 4: quantize_heads' 4-bit levels of the
+ *              rotated query (Table 3's 4-bit Q), eps its epsilon
+ *   O          device, bfloat16 [T, Hq, D], dense, 16-byte aligned
+ *   workspace  kv_pages_attention_workspace_bytes(T, n_seqs, Hq, H, D, max_pages) bytes, 16-byte aligned (may be 0: then NULL); what a
+ *              call leaves there means nothing to the next, but calls that may overlap in time need one each
+ *   Probabilities are rounded to 8 significand bits for the second product; sums, maxima and outputs are float32 until the end.
+ * Errors: BL_EINVAL (null pointer, enum, sizes < 1, Hq % H, scale not positive and finite, eps < 0, window or sinks < 0, strides),
+ * BL_ESHAPE (D, n_pos, sizes), BL_EALIGN, BL_EWORKSPACE. */
+#define BL_KV_PAGE 128
+size_t kv_page_bytes(int64_t H, int64_t D);
+int kv_pages_append(const void* K, int64_t ldk, const void* V, int64_t ldv, bl_dtype x_dtype, int64_t T, int64_t H, int64_t D,
+                    const int32_t* q_start, const int32_t* kv_len, int64_t n_seqs, const int32_t* page_table, int64_t max_pages,
+                    const float* rope, int64_t n_pos, float eps, void* pages, int64_t n_pages, void* stream);
+int kv_pages_read(const void* pages, int64_t n_pages, const int32_t* q_start, const int32_t* kv_len, int64_t n_seqs,
+                  const int32_t* page_table, int64_t max_pages, int64_t T, int64_t H, int64_t D, void* K_out, void* V_out,
+                  bl_dtype out_dtype, void* stream);
+size_t kv_pages_attention_workspace_bytes(int64_t T, int64_t n_seqs, int64_t Hq, int64_t H, int64_t D, int64_t max_pages);
+int kv_pages_attention(const void* Q, int64_t ldq, bl_dtype q_dtype, int64_t T, int64_t Hq, int64_t H, int64_t D, int q_bits,
+                       const int32_t* q_start, const int32_t* kv_len, int64_t n_seqs, const int32_t* page_table, int64_t max_pages,
+                       const float* rope, int64_t n_pos, float scale, float eps, int64_t window, int64_t sinks, const void* pages,
+                       int64_t n_pages, void* O, void* workspace, size_t workspace_bytes, void* stream);
+
+/* RMS norm in front of a quantized linear: the residual stream's addition, the norm and the codes of the result in one launch.
+ *     h = X + R (one rounding to dtype; R NULL: h = X);  rstd = 1 / sqrt(mean(h^2) + norm_eps)  (float64, one rounding to float32)
+ *     y = (h * rstd) * gamma  (two float32 multiplies);  codes and scale of y as quantize_act gives them for float32 rows y
+ *   X, R       device, [M, K] of dtype;  gamma device, float32 [K]
+ *   mode       BL_ACT_INT4_ABSMEAN, BL_ACT_INT4_ABSMEAN_MX6, or BL_ACT_TOPK_INT8_ABSMAX with every channel kept (topk = K); others:
+ *              BL_EUNSUPPORTED.  q_out and scale_out as quantize_act's, for bitlinear_gemm, bitlinear_gemm_glu, bitlinear_backward.
+ *   H_out      nullable; device, [M, K] of dtype: h (may be X or R itself)
+ *   rstd_out   nullable; device, float32 [M], for rmsnorm_backward */
+int rmsnorm_quantize(const void* X, const void* R, bl_dtype dtype, int64_t M, int64_t K, const float* gamma, float norm_eps,
+                     bl_act_mode mode, float eps, void* H_out, float* rstd_out, void* q_out, float* scale_out, void* stream);
+
+/* Gradient of the norm above under the straight-through estimator (the quantizer passed over).  dY is the gradient at y (what
+ * bitlinear_backward gives as dX), dH, nullable, the gradient that reaches h another way (the residual stream):
+ *     xh = h * rstd,  a = dY * gamma,  dX = dH + rstd * (a - xh * mean(a * xh)),  dgamma[k] = sum over tokens of dY * xh
+ * dX is the gradient for X and for R alike.  Float32, sums over tokens in a fixed order.
+ *   dY, H, dH, dX  device, [M, K] of dtype (dX may be dY or dH itself);  rstd float32 [M];  gamma, dgamma float32 [K] (dgamma is
+ *              overwritten);  workspace rmsnorm_backward_workspace_bytes(M, K) bytes, 16-byte aligned */
+size_t rmsnorm_backward_workspace_bytes(int64_t M, int64_t K);
+int rmsnorm_backward(const void* dY, const void* H, const float* rstd, const float* gamma, const void* dH, bl_dtype dtype, int64_t M,
+                     int64_t K, void* dX, float* dgamma, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Backward pass of a quantized linear layer under the straight-through estimator (Section 2.2,
  * "Gradient approximation": the quantization functions and the top-K function are passed over).  With
  * the forward pass's dequantized operands Xq[m, k] = scale[m] * q[m, k] (zeros where Top_k masked) and

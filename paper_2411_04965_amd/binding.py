@@ -63,6 +63,16 @@ _SIGNATURES = {
     "kv_cache_bytes": (_sz, [_i64, _i64, _i64]),
     "kv_cache_append": (_int, [_vp, _int, _i64, _i64, _i64, _i64, _f32, _vp, _vp, _vp]),
     "kv_cache_read": (_int, [_vp, _vp, _i64, _i64, _i64, _i64, _vp, _int, _vp]),
+    "kv_page_bytes": (_sz, [_i64, _i64]),
+    "kv_pages_append": (_int, [_vp, _i64, _vp, _i64, _int, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _f32, _vp, _i64,
+                               _vp]),
+    "kv_pages_read": (_int, [_vp, _i64, _vp, _vp, _i64, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _int, _vp]),
+    "kv_pages_attention_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64, _i64, _i64]),
+    "kv_pages_attention": (_int, [_vp, _i64, _int, _i64, _i64, _i64, _i64, _int, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _f32, _f32,
+                                  _i64, _i64, _vp, _i64, _vp, _vp, _sz, _vp]),
+    "rmsnorm_quantize": (_int, [_vp, _vp, _int, _i64, _i64, _vp, _f32, _int, _f32, _vp, _vp, _vp, _vp, _vp]),
+    "rmsnorm_backward_workspace_bytes": (_sz, [_i64, _i64]),
+    "rmsnorm_backward": (_int, [_vp, _vp, _vp, _vp, _vp, _int, _i64, _i64, _vp, _vp, _vp, _sz, _vp]),
     "quantize_act_glu": (_int, [_vp, _vp, _int, _i64, _i64, _i64, _f32, _vp, _vp, _vp, _vp]),
     "bitlinear_gate_up_workspace_bytes": (_sz, [_i64, _i64, _i64, _int]),
     "bitlinear_a4_gate_up": (_int, [_vp, _int, _i64, _i64, _vp, _vp, _vp, _vp, _int, _i64, _f32, _vp, _vp, _int,
@@ -164,6 +174,24 @@ def _dev(t):
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError("contiguous device tensor expected")
     return t
+
+
+class _Here:
+    """Nothing to switch: the tensors are on the current device."""
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        return False
+
+
+_here = _Here()
+
+
+def _on(t):
+    """Makes a tensor's device the current one for a call (and its current stream the call's)."""
+    return _here if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
 
 
 def noop():
@@ -390,6 +418,145 @@ def kv_cache_read(cache, scales, pos0, T, H, D, out_dtype=torch.float32):
     out = torch.empty((T, H, D), dtype=out_dtype, device=cache.device)
     _check("kv_cache_read", lib().kv_cache_read(_ptr(cache), _ptr(scales), pos0, T, H, D, _ptr(out), _dt(out), _stream()))
     return out
+
+
+def _rows(x):
+    """[T, H, D] device tensor whose rows may be a stride apart (a slice of a fused product's output) -> the stride."""
+    if not x.is_cuda or x.dim() != 3:
+        raise ValueError("device tensor [T, H, D] expected")
+    if x.shape[2] > 1 and x.stride(2) != 1 or x.shape[1] > 1 and x.stride(1) != x.shape[2]:
+        raise ValueError("dense heads expected: strides %s for shape %s" % (tuple(x.stride()), tuple(x.shape)))
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * x.shape[2]
+
+
+def _batch(pages, page_table, q_start, kv_len, rope, H, D, T):
+    """Checks what the paged calls share; -> (n_pages, n_seqs, max_pages, n_pos)."""
+    for t in (page_table, q_start, kv_len):
+        if _dev(t).dtype != torch.int32:
+            raise TypeError("int32 tensor expected, got %s" % t.dtype)
+    n_seqs = kv_len.numel()
+    if page_table.dim() != 2 or page_table.shape[0] != n_seqs or q_start.numel() != n_seqs + 1:
+        raise ValueError("page_table [n_seqs, max_pages], q_start [n_seqs + 1] and kv_len [n_seqs] expected")
+    if _dev(pages).dtype != torch.uint8 or pages.dim() != 2 or pages.shape[1] != lib().kv_page_bytes(H, D):
+        raise ValueError("pages of kv_pages_new for %d heads of %d expected" % (H, D))
+    if rope is not None and (_dev(rope).dtype != torch.float32 or rope.dim() != 2 or rope.shape[1] != D):
+        raise ValueError("float32 rope table [positions, %d] expected" % D)
+    for t in (page_table, q_start, kv_len, rope):
+        if t is not None and t.device != pages.device:
+            raise ValueError("tensors on one device expected")
+    return pages.shape[0], n_seqs, page_table.shape[1], 0 if rope is None else rope.shape[0]
+
+
+def kv_pages_new(n_pages, H, D, device):
+    """A pool of empty pages (128 positions each, keys and values of H heads of D channels)."""
+    n = lib().kv_page_bytes(H, D)
+    if n == 0:
+        raise BitlinearError("kv_page_bytes", -2)
+    return torch.zeros((n_pages, n), dtype=torch.uint8, device=device)
+
+
+def kv_pages_append(K, V, pages, page_table, q_start, kv_len, rope=None, eps=DEFAULT_EPS):
+    """Quantizes K (rotated where `rope` is given) and V [T, H, D] into their pages: rows q_start[s] .. q_start[s + 1] - 1 are the
+    last positions of sequence s, whose length with them is kv_len[s].  Rows may be a stride apart."""
+    ldk, ldv = _rows(K), _rows(V)
+    if K.shape != V.shape or K.dtype != V.dtype or K.device != pages.device or V.device != pages.device:
+        raise ValueError("K and V of one shape, type and device expected")
+    T, H, D = K.shape
+    n_pages, n_seqs, max_pages, n_pos = _batch(pages, page_table, q_start, kv_len, rope, H, D, T)
+    with _on(pages):
+        _check("kv_pages_append", lib().kv_pages_append(
+            _ptr(K), ldk, _ptr(V), ldv, _dt(K), T, H, D, _ptr(q_start), _ptr(kv_len), n_seqs, _ptr(page_table), max_pages, _ptr(rope),
+            n_pos, eps, _ptr(pages), n_pages, _stream()))
+
+
+def kv_pages_read(pages, page_table, q_start, kv_len, T, H, D, out_dtype=torch.float32, out=None):
+    """The values of the batch's rows -> (K, V) [T, H, D]; `out` may bring the pair (rows of no sequence stay as they are there)."""
+    n_pages, n_seqs, max_pages, _ = _batch(pages, page_table, q_start, kv_len, None, H, D, T)
+    K, V = out if out is not None else (torch.zeros((T, H, D), dtype=out_dtype, device=pages.device) for _ in range(2))
+    for t in (K, V):
+        if tuple(_dev(t).shape) != (T, H, D) or t.dtype != K.dtype or t.device != pages.device:
+            raise ValueError("outputs [T, H, D] of one type expected")
+    with _on(pages):
+        _check("kv_pages_read", lib().kv_pages_read(
+            _ptr(pages), n_pages, _ptr(q_start), _ptr(kv_len), n_seqs, _ptr(page_table), max_pages, T, H, D, _ptr(K), _ptr(V), _dt(K),
+            _stream()))
+    return K, V
+
+
+def kv_pages_attention(Q, pages, page_table, q_start, kv_len, H, rope=None, scale=None, window=0, sinks=0, q_bits=16,
+                       eps=DEFAULT_EPS, ws=None, out=None):
+    """Causal attention of the batch's rows Q [T, Hq, D] over the cache's H heads -> O bfloat16 [T, Hq, D].  scale: D^-0.5 if None;
+    window > 0: a row sees its last `window` positions and the sequence's first `sinks`."""
+    ldq = _rows(Q)
+    T, Hq, D = Q.shape
+    if Q.device != pages.device:
+        raise ValueError("tensors on one device expected")
+    n_pages, n_seqs, max_pages, n_pos = _batch(pages, page_table, q_start, kv_len, rope, H, D, T)
+    L = lib()
+    n = L.kv_pages_attention_workspace_bytes(T, n_seqs, Hq, H, D, max_pages)
+    if ws is None and n:
+        ws = torch.empty(n, dtype=torch.uint8, device=Q.device)
+    O = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=Q.device) if out is None else out
+    if _dev(O).dtype != torch.bfloat16 or O.shape != Q.shape or O.device != Q.device:
+        raise ValueError("bfloat16 output [T, Hq, D] expected")
+    with _on(pages):
+        _check("kv_pages_attention", L.kv_pages_attention(
+            _ptr(Q), ldq, _dt(Q), T, Hq, H, D, q_bits, _ptr(q_start), _ptr(kv_len), n_seqs, _ptr(page_table), max_pages, _ptr(rope),
+            n_pos, D ** -0.5 if scale is None else scale, eps, window, sinks, _ptr(pages), n_pages, _ptr(O), _ptr(ws),
+            0 if ws is None else ws.numel() * ws.element_size(), _stream()))
+    return O
+
+
+def _same(ref, *tensors):
+    """Tensors of ref's shape, type and device (None: not given)."""
+    for t in tensors:
+        if t is not None and (_dev(t).shape != ref.shape or t.dtype != ref.dtype or t.device != ref.device):
+            raise ValueError("tensors of one shape, type and device expected")
+
+
+def _per(t, n, device):
+    if _dev(t).dtype != torch.float32 or t.numel() != n or t.device != device:
+        raise ValueError("float32 tensor of %d values on %s expected" % (n, device))
+
+
+def rmsnorm_quantize(X, gamma, mode, residual=None, norm_eps=1e-5, eps=DEFAULT_EPS):
+    """h = X (+ residual), RMS norm with weights gamma, codes of the result in `mode` -> dict(q, scale, h, rstd); q and scale as
+    quantize_act's (BL_ACT_TOPK_INT8_ABSMAX keeps every channel); h is X itself where there is no residual."""
+    _dev(X)
+    M, K = X.shape
+    _same(X, residual)
+    _per(gamma, K, X.device)
+    L = lib()
+    q = torch.empty(L.quantize_act_bytes(mode, M, K), dtype=torch.uint8, device=X.device)
+    scale = torch.empty(M, dtype=torch.float32, device=X.device)
+    rstd = torch.empty(M, dtype=torch.float32, device=X.device)
+    h = X if residual is None else torch.empty_like(X)
+    with _on(X):
+        _check("rmsnorm_quantize", L.rmsnorm_quantize(
+            _ptr(X), _ptr(residual), _dt(X), M, K, _ptr(gamma), norm_eps, mode, eps, None if residual is None else _ptr(h), _ptr(rstd),
+            _ptr(q), _ptr(scale), _stream()))
+    return dict(q=q, scale=scale, h=h, rstd=rstd)
+
+
+def rmsnorm_backward(dY, H, rstd, gamma, dH=None, ws=None):
+    """Gradient of the norm: dY [M, K] at its output, H and rstd from the forward pass, dH the residual stream's own gradient
+    -> (dX like H, dgamma float32 [K])."""
+    _dev(H)
+    M, K = H.shape
+    _same(H, dY, dH)
+    _per(gamma, K, H.device)
+    _per(rstd, M, H.device)
+    L = lib()
+    n = L.rmsnorm_backward_workspace_bytes(M, K)
+    if ws is None:
+        ws = torch.empty(n, dtype=torch.uint8, device=H.device)
+    dX = torch.empty_like(H)
+    dgamma = torch.empty(K, dtype=torch.float32, device=H.device)
+    with _on(H):
+        _check("rmsnorm_backward", L.rmsnorm_backward(
+            _ptr(dY), _ptr(H), _ptr(rstd), _ptr(gamma), _ptr(dH), _dt(H), M, K, _ptr(dX), _ptr(dgamma), _ptr(ws),
+            ws.numel() * ws.element_size(), _stream()))
+    return dX, dgamma
 
 
 def bitlinear_backward(dY, q, scale, mode, K, W_kmajor, alpha, want_dx=True, want_dw=True,

@@ -1,6 +1,7 @@
 // C ABI of the library: argument validation and kernel dispatch.  See include/bitlinear.h for
 // the contract of every entry point.
 #include "common.h"
+#include "kv_pages.h"
 
 #include <mutex>
 
@@ -240,6 +241,121 @@ extern "C" int kv_cache_read(const void* cache, const float* scales, int64_t pos
   if (!bl_aligned16(out)) return BL_EALIGN;
   return bl_launch_dequantize_heads((const unsigned char*)cache + kv_token_offset(pos0, H, D), scales + pos0 * H, T * H,
                                     pos0 == 0 ? H : 0, D, 3, out, out_dtype, (hipStream_t)stream);
+}
+
+// ---------------------------------------------------------------- paged cache and attention over it
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+
+extern "C" size_t kv_page_bytes(int64_t H, int64_t D) {
+  if (H < 1 || H > (1 << 20) || D < 2 || D > KP_MAX_D || D % 2 != 0) return 0;
+  return (size_t)H * kp_head_bytes(kp_units((int)D));
+}
+
+// what the three calls check alike
+static int kv_pages_check(int64_t T, int64_t H, int64_t D, const int32_t* q_start, const int32_t* kv_len, int64_t n_seqs,
+                          const int32_t* table, int64_t max_pages, const float* rope, int64_t n_pos, const void* pages, int64_t n_pages) {
+  if (!q_start || !kv_len || !table || !pages) return BL_EINVAL;
+  if (T < 1 || H < 1 || D < 1 || n_seqs < 1 || max_pages < 1 || n_pages < 1) return BL_EINVAL;
+  if (kv_page_bytes(H, D) == 0) return BL_ESHAPE;
+  const int64_t lim = ((int64_t)1 << 31) - 1;
+  // (positions are 32-bit numbers; rows and sequences bound the grids below)
+  if (T > lim / 2 || n_seqs > lim / 4 || max_pages > lim / KP_TOKENS || n_pages > lim || n_seqs > ((int64_t)1 << 40) / max_pages) return BL_ESHAPE;
+  if (rope && n_pos < max_pages * KP_TOKENS) return BL_ESHAPE;
+  if (!aligned4(q_start) || !aligned4(kv_len) || !aligned4(table) || !aligned4(rope) || (reinterpret_cast<uintptr_t>(pages) & 127)) return BL_EALIGN;
+  return BL_OK;
+}
+static KvBatch kv_batch(const int32_t* q_start, const int32_t* kv_len, int64_t n_seqs, const int32_t* table, int64_t max_pages,
+                        int64_t n_pages, int64_t T) {
+  return KvBatch{q_start, kv_len, table, (int)n_seqs, (int)max_pages, (int)n_pages, (int)T};
+}
+// rows of `heads` dense heads, a stride apart
+static bool kv_rows_ok(int64_t T, int64_t heads, int64_t D, int64_t ld) {
+  return ld >= heads * D && ld <= ((int64_t)1 << 40) / T;
+}
+
+extern "C" int kv_pages_append(const void* K, int64_t ldk, const void* V, int64_t ldv, bl_dtype x_dtype, int64_t T, int64_t H, int64_t D,
+                               const int32_t* q_start, const int32_t* kv_len, int64_t n_seqs, const int32_t* page_table,
+                               int64_t max_pages, const float* rope, int64_t n_pos, float eps, void* pages, int64_t n_pages,
+                               void* stream) {
+  if (!K || !V || !valid_dtype(x_dtype) || !(eps >= 0.0f)) return BL_EINVAL;
+  int rc = kv_pages_check(T, H, D, q_start, kv_len, n_seqs, page_table, max_pages, rope, n_pos, pages, n_pages);
+  if (rc) return rc;
+  if (!kv_rows_ok(T, H, D, ldk) || !kv_rows_ok(T, H, D, ldv)) return BL_EINVAL;
+  if (!bl_aligned16(K) || !bl_aligned16(V)) return BL_EALIGN;
+  return bl_launch_kv_append(K, ldk, V, ldv, x_dtype, (int)H, (int)D, kv_batch(q_start, kv_len, n_seqs, page_table, max_pages, n_pages, T),
+                             rope, n_pos, eps, pages, (hipStream_t)stream);
+}
+
+extern "C" int kv_pages_read(const void* pages, int64_t n_pages, const int32_t* q_start, const int32_t* kv_len, int64_t n_seqs,
+                             const int32_t* page_table, int64_t max_pages, int64_t T, int64_t H, int64_t D, void* K_out, void* V_out,
+                             bl_dtype out_dtype, void* stream) {
+  if ((!K_out && !V_out) || !valid_dtype(out_dtype)) return BL_EINVAL;
+  int rc = kv_pages_check(T, H, D, q_start, kv_len, n_seqs, page_table, max_pages, nullptr, 0, pages, n_pages);
+  if (rc) return rc;
+  if (!kv_rows_ok(T, H, D, H * D)) return BL_ESHAPE;
+  if ((K_out && !bl_aligned16(K_out)) || (V_out && !bl_aligned16(V_out))) return BL_EALIGN;
+  return bl_launch_kv_read(pages, (int)H, (int)D, kv_batch(q_start, kv_len, n_seqs, page_table, max_pages, n_pages, T), K_out, V_out,
+                           out_dtype, (hipStream_t)stream);
+}
+
+extern "C" size_t kv_pages_attention_workspace_bytes(int64_t T, int64_t n_seqs, int64_t Hq, int64_t H, int64_t D, int64_t max_pages) {
+  const int64_t lim = ((int64_t)1 << 31) - 1;
+  if (T < 1 || n_seqs < 1 || H < 1 || Hq < H || Hq % H != 0 || Hq > (1 << 20) || D < 1 || D > KP_MAX_D || max_pages < 1) return 0;
+  if (T > lim / 2 || n_seqs > lim / 4 || max_pages > lim) return 0;
+  return bl_kv_attention_ws_bytes(T, n_seqs, Hq / H, H, D, max_pages);
+}
+
+extern "C" int kv_pages_attention(const void* Q, int64_t ldq, bl_dtype q_dtype, int64_t T, int64_t Hq, int64_t H, int64_t D, int q_bits,
+                                  const int32_t* q_start, const int32_t* kv_len, int64_t n_seqs, const int32_t* page_table,
+                                  int64_t max_pages, const float* rope, int64_t n_pos, float scale, float eps, int64_t window,
+                                  int64_t sinks, const void* pages, int64_t n_pages, void* O, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  if (!Q || !O || !valid_dtype(q_dtype) || (q_bits != 16 && q_bits != 4) || !(eps >= 0.0f)) return BL_EINVAL;
+  if (!(scale > 0.0f) || scale > 3.0e38f || window < 0 || sinks < 0) return BL_EINVAL;
+  int rc = kv_pages_check(T, H, D, q_start, kv_len, n_seqs, page_table, max_pages, rope, n_pos, pages, n_pages);
+  if (rc) return rc;
+  if (Hq < H || Hq % H != 0) return BL_EINVAL;
+  if (Hq > (1 << 20) || T > (((int64_t)1 << 31) - 1) / (Hq / H)) return BL_ESHAPE;
+  if (!kv_rows_ok(T, Hq, D, ldq)) return BL_EINVAL;
+  if (!bl_aligned16(Q) || !bl_aligned16(O)) return BL_EALIGN;
+  const size_t need = bl_kv_attention_ws_bytes(T, n_seqs, Hq / H, H, D, max_pages);
+  if (need && (!workspace || workspace_bytes < need)) return BL_EWORKSPACE;
+  if (need && !bl_aligned16(workspace)) return BL_EALIGN;
+  return bl_launch_kv_attention(Q, ldq, q_dtype, (int)Hq, (int)H, (int)D, q_bits,
+                                kv_batch(q_start, kv_len, n_seqs, page_table, max_pages, n_pages, T), rope, n_pos, scale, eps, window,
+                                sinks, pages, O, workspace, (hipStream_t)stream);
+}
+
+// ---------------------------------------------------------------- RMS norm
+extern "C" int rmsnorm_quantize(const void* X, const void* R, bl_dtype dtype, int64_t M, int64_t K, const float* gamma, float norm_eps,
+                                bl_act_mode mode, float eps, void* H_out, float* rstd_out, void* q_out, float* scale_out, void* stream) {
+  if (!X || !gamma || !q_out || !scale_out) return BL_EINVAL;
+  if (!valid_dtype(dtype) || !valid_mode(mode) || !(eps >= 0.0f) || !(norm_eps >= 0.0f)) return BL_EINVAL;
+  int rc = check_sizes(M, 1, K);
+  if (rc) return rc;
+  if (mode != BL_ACT_INT4_ABSMEAN && mode != BL_ACT_INT4_ABSMEAN_MX6 && mode != BL_ACT_TOPK_INT8_ABSMAX) return BL_EUNSUPPORTED;
+  if (!bl_grid_ok(bl_round_up(M, 8)) || M > ((int64_t)1 << 40) / K) return BL_ESHAPE;
+  if (!bl_aligned16(X) || (R && !bl_aligned16(R)) || (H_out && !bl_aligned16(H_out)) || !bl_aligned16(q_out)) return BL_EALIGN;
+  if (!aligned4(gamma) || !aligned4(rstd_out) || !aligned4(scale_out)) return BL_EALIGN;
+  return bl_launch_rmsnorm_quantize(X, R, dtype, M, K, gamma, norm_eps, mode, eps, H_out, rstd_out, q_out, scale_out, (hipStream_t)stream);
+}
+
+extern "C" size_t rmsnorm_backward_workspace_bytes(int64_t M, int64_t K) {
+  if (M < 1 || K < 1 || K > BL_MAX_K) return 0;
+  return bl_rmsnorm_backward_ws_bytes(M, K);
+}
+
+extern "C" int rmsnorm_backward(const void* dY, const void* H, const float* rstd, const float* gamma, const void* dH, bl_dtype dtype,
+                                int64_t M, int64_t K, void* dX, float* dgamma, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!dY || !H || !rstd || !gamma || !dX || !dgamma || !valid_dtype(dtype)) return BL_EINVAL;
+  int rc = check_sizes(M, 1, K);
+  if (rc) return rc;
+  if (M > ((int64_t)1 << 40) / K) return BL_ESHAPE;
+  if (!bl_aligned16(dY) || !bl_aligned16(H) || (dH && !bl_aligned16(dH)) || !bl_aligned16(dX)) return BL_EALIGN;
+  if (!aligned4(rstd) || !aligned4(gamma) || !aligned4(dgamma)) return BL_EALIGN;
+  if (!workspace || workspace_bytes < bl_rmsnorm_backward_ws_bytes(M, K)) return BL_EWORKSPACE;
+  if (!bl_aligned16(workspace)) return BL_EALIGN;
+  return bl_launch_rmsnorm_backward(dY, H, rstd, gamma, dH, dtype, M, K, dX, dgamma, workspace, (hipStream_t)stream);
 }
 
 // ---------------------------------------------------------------- ReLU^2 GLU (eq. 5)

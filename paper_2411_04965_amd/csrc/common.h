@@ -276,4 +276,17 @@ int bl_launch_gemm_decode_glu(const void* q, const float* scale, int64_t M, int6
 bool bl_gemv_stream_glu_codes_ok(int64_t M, int64_t N, int64_t K);
 int bl_launch_gemv_stream_glu_codes(const void* q, const float* scale, int64_t M, int64_t K, const void* Wg,
                                     const float* ag, const void* Wu, const float* au, int64_t N, void* H, hipStream_t s);
-
+// paged cache, attention over it, norm (kv_pages.hip, kv_attention.hip, rmsnorm.hip)
+struct KvBatch;
+int bl_launch_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv, bl_dtype dt, int H, int D, const KvBatch& b,
+                        const float* rope, int64_t n_pos, float eps, void* pages, hipStream_t s);
+int bl_launch_kv_read(const void* pages, int H, int D, const KvBatch& b, void* K, void* V, bl_dtype odt, hipStream_t s);
+size_t bl_kv_attention_ws_bytes(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t D, int64_t max_pages);
+int bl_launch_kv_attention(const void* Q, int64_t ldq, bl_dtype qdt, int Hq, int H, int D, int q_bits, const KvBatch& b,
+                           const float* rope, int64_t n_pos, float scale, float eps, int64_t window, int64_t sinks,
+                           const void* pages, void* O, void* ws, hipStream_t s);
+int bl_launch_rmsnorm_quantize(const void* X, const void* R, bl_dtype dt, int64_t M, int64_t K, const float* gamma, float norm_eps,
+                               bl_act_mode mode, float eps, void* H, float* rstd, void* q, float* scale, hipStream_t s);
+size_t bl_rmsnorm_backward_ws_bytes(int64_t M, int64_t K);
+int bl_launch_rmsnorm_backward(const void* dY, const void* H, const float* rstd, const float* gamma, const void* dH, bl_dtype dt,
+                               int64_t M, int64_t K, void* dX, float* dgamma, void* ws, hipStream_t s);

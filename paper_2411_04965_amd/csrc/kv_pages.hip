@@ -1,0 +1,298 @@
+// The paged form of the low-bit key / value cache (Section 4.2, Table 3): a batch's new keys and values are rotated (keys),
+// quantized per head to 3 bits, or 4 at position 0, and put into their places; and the way back.
+//   gamma = max |x| over the head,  q = RoundClip(x * (Q_b / (gamma + eps)), -Q_b, Q_b),  scale = gamma / Q_b
+// HBM bound: 2 D bytes of a bfloat16 head in, 3 D / 8 + 4 out.
+//
+// Workgroup = one head of one page.  Key codes are a token's own 12 byte groups.  Value codes of 32 tokens share words, so the
+// page's new tokens are coded into LDS first and the words are then put together by one thread each, the bits of older tokens
+// kept: no two workgroups write the same word, and no order of anything decides what is stored.
+#include "kv_pages.h"
+
+#define KP_THREADS 256
+
+template <typename RawT>
+__device__ __forceinline__ float kp_to_f32(RawT v) {
+  return sizeof(RawT) == 2 ? __uint_as_float((u32)v << 16) : __uint_as_float((u32)v);
+}
+
+// 8 channels from c on of a head of D channels (zeros behind it)
+template <typename RawT, bool VEC>
+__device__ __forceinline__ void kp_load8(const RawT* x, int c, int D, float (&v)[8]) {
+  if (VEC) {                                     // D % 16 == 0, 16-byte aligned
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+    if (c < D) {
+      if (sizeof(RawT) == 2) {
+        const uint4 w = *reinterpret_cast<const uint4*>(x + c);
+        const u32 ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[2 * e] = __uint_as_float(ww[e] << 16);
+          v[2 * e + 1] = __uint_as_float(ww[e] & 0xFFFF0000u);
+        }
+      } else {
+        const float4 a = *reinterpret_cast<const float4*>(x + c), b = *reinterpret_cast<const float4*>(x + c + 4);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c + e < D ? kp_to_f32<RawT>(x[c + e]) : 0.0f;
+  }
+}
+
+// LPT lanes a token, 8 channels a lane
+template <int LPT>
+__device__ __forceinline__ float kp_head_max(const float (&v)[8]) {
+  float m = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[e]));
+#pragma unroll
+  for (int o = 1; o < LPT; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  return m;
+}
+
+// levels of 8 channels as bytes: bits 0, 1 stored magnitude, bit 2 sign, bit 3 the lowest magnitude bit of a 4-bit level
+__device__ __forceinline__ void kp_levels8(const float (&v)[8], float s, float qb, bool four, u32 (&lv)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float p = fminf(fmaxf(rintf(v[e] * s), -qb), qb);     // one float32 multiply
+    const u32 m = (u32)fabsf(p), sg = p < 0.0f ? 4u : 0u;
+    lv[e] = four ? (m >> 1) | sg | ((m & 1u) << 3) : m | sg;
+  }
+}
+
+template <typename RawT, int LPT, bool VEC>
+__global__ __launch_bounds__(KP_THREADS) void kv_append_kernel(
+    const RawT* __restrict__ K, int64_t ldk, const RawT* __restrict__ V, int64_t ldv, int H, int D, KvBatch b,
+    const float* __restrict__ rope, int64_t n_pos, float eps, unsigned char* __restrict__ pages) {
+  constexpr int ROW = 8 * LPT;                   // LDS bytes a token
+  __shared__ __align__(16) unsigned char vq[KP_TOKENS * ROW];
+  const int h = (int)(blockIdx.x % (unsigned)H);
+  KvSeq q;
+  const int64_t local = kp_find(b, blockIdx.x / (unsigned)H, 1, 7, 2, q);
+  if (local < 0) return;
+  const int64_t pg = (q.pos0 > 0 ? q.pos0 >> 7 : 0) + local;
+  if (pg >= b.max_pages || pg * KP_TOKENS >= q.len) return;
+  const int id = b.table[(int64_t)q.s * b.max_pages + pg];
+  if (id < 0 || id >= b.n_pages) return;
+  // tokens a .. e - 1 of the page are new
+  const int a = (int)max(q.pos0 - pg * KP_TOKENS, (int64_t)0), e = (int)min(q.len - pg * KP_TOKENS, (int64_t)KP_TOKENS);
+  const int U = kp_units(D), Dp = 32 * U, half = D >> 1;
+  unsigned char* head = pages + ((int64_t)id * H + h) * kp_head_bytes(U);
+  float* k_scale = reinterpret_cast<float*>(head + kp_scale_off(U));
+  float* v_scale = k_scale + KP_TOKENS;
+  u32* lows = reinterpret_cast<u32*>(head + kp_low_off(U));
+  const int j = threadIdx.x % LPT, c = 8 * j, jq = j & 3, u = j >> 2;
+
+  for (int base = a; base < e; base += KP_THREADS / LPT) {      // (every lane stays: the quads exchange words)
+    const int tok = base + (int)threadIdx.x / LPT;
+    const bool have = tok < e;
+    const int64_t pos = pg * KP_TOKENS + tok;
+    const int64_t row = have ? q.q0 + (pos - q.pos0) : q.q0;
+    const bool four = pos == 0;
+    const float qb = four ? 7.0f : 3.0f;
+    float v[8];
+    u32 lv[8];
+    // key
+    const RawT* x = K + row * ldk + (int64_t)h * D;
+    kp_load8<RawT, VEC>(x, c, D, v);
+    if (rope) {
+      const float* rr = rope + min(pos, n_pos - 1) * D;
+      float o[8];
+      if (VEC) {
+        kp_load8<RawT, true>(x, c < half ? c + half : c - half, D, o);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (c < D) v[i] = kp_rotate(v[i], o[i], rr, c + i, half);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (c + i < D) v[i] = kp_rotate(v[i], kp_to_f32<RawT>(x[c + i < half ? c + i + half : c + i - half]), rr, c + i, half);
+      }
+    }
+    float g = kp_head_max<LPT>(v);
+    kp_levels8(v, qb / (g + eps), qb, four, lv);
+    if (have && j == 0) k_scale[tok] = g / qb;
+    u32 mag = 0, sgn = 0, low = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      mag |= (lv[i] & 3u) << (4 * i);
+      sgn |= ((lv[i] >> 2) & 1u) << (4 * i);
+      low |= (lv[i] >> 3) << (4 * i);
+    }
+    mag <<= 2 * (jq & 1);
+    sgn <<= 3 - jq;
+    low <<= 3 - jq;
+    auto quad = [](u32 w, auto ctrl) { return (u32)__builtin_amdgcn_update_dpp(0, (int)w, decltype(ctrl)::value, 0xF, 0xF, false); };
+    mag |= quad(mag, std::integral_constant<int, 0xB1>{});                  // lanes 0, 1: A; lanes 2, 3: B
+    const u32 magB = quad(mag, std::integral_constant<int, 0xAA>{});        // B in every lane
+    sgn |= quad(sgn, std::integral_constant<int, 0xB1>{});
+    sgn |= quad(sgn, std::integral_constant<int, 0x4E>{});
+    low |= quad(low, std::integral_constant<int, 0xB1>{});
+    low |= quad(low, std::integral_constant<int, 0x4E>{});
+    if (have && u < U) {
+      u32* w = reinterpret_cast<u32*>(head) + (kp_slot(tok) * U + u) * 3;
+      if (jq < 3) w[jq] = jq == 0 ? mag : jq == 1 ? magB : sgn;
+      if (four && jq == 3) lows[u] = low;
+    }
+    // value
+    kp_load8<RawT, VEC>(V + row * ldv + (int64_t)h * D, c, D, v);
+    g = kp_head_max<LPT>(v);
+    kp_levels8(v, qb / (g + eps), qb, four, lv);
+    if (have) {
+      if (j == 0) v_scale[tok] = g / qb;
+      uint2 w = make_uint2(0u, 0u);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        w.x |= lv[i] << (8 * i);
+        w.y |= lv[4 + i] << (8 * i);
+      }
+      *reinterpret_cast<uint2*>(vq + tok * ROW + c) = w;
+    }
+  }
+  __syncthreads();
+  if (pg == 0 && a == 0 && (int)threadIdx.x < U) {
+    u32 w = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) w |= (u32)((vq[32 * threadIdx.x + i] >> 3) & 1) << kp_sign_bit(i);
+    lows[U + threadIdx.x] = w;
+  }
+  for (int it = threadIdx.x; it < 4 * Dp; it += KP_THREADS) {
+    const int g = it / Dp, d = it - g * Dp;
+    const int lo = max(a - 32 * g, 0), hi = min(e - 32 * g, 32);            // tokens lo .. hi - 1 of the 32
+    if (lo >= hi) continue;
+    u32* w = reinterpret_cast<u32*>(head + kp_code_bytes(U)) + (d * 4 + g) * 3;
+    u32 nw[3] = {0u, 0u, 0u}, keep[3] = {~0u, ~0u, ~0u};
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      if (i >= lo && i < hi) {
+        const u32 v = vq[(32 * g + i) * ROW + d];
+        nw[i >> 4] |= (v & 3u) << kp_mag_bit(i);
+        nw[2] |= ((v >> 2) & 1u) << kp_sign_bit(i);
+        keep[i >> 4] &= ~(3u << kp_mag_bit(i));
+        keep[2] &= ~(1u << kp_sign_bit(i));
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (keep[k] != ~0u) w[k] = keep[k] ? (w[k] & keep[k]) | nw[k] : nw[k];
+  }
+}
+
+// Work items of the two kernels here: pages that hold rows of the call, at most two more a sequence than whole pages of rows.
+static int64_t kp_items(int64_t T, int64_t n_seqs) { return (T >> 7) + 2 * n_seqs; }
+
+int bl_launch_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv, bl_dtype dt, int H, int D, const KvBatch& b,
+                        const float* rope, int64_t n_pos, float eps, void* pages, hipStream_t s) {
+  const int64_t blocks = kp_items(b.T, b.n_seqs) * H;
+  if (!bl_grid_ok(blocks)) return BL_ESHAPE;
+  const int es = dt == BL_BF16 ? 2 : 4;
+  const bool vec = D % 16 == 0 && bl_aligned16(K) && bl_aligned16(V) && ldk * es % 16 == 0 && ldv * es % 16 == 0;
+#define KP_GO(T, LPT, VEC) \
+  kv_append_kernel<T, LPT, VEC><<<(unsigned)blocks, KP_THREADS, 0, s>>>((const T*)K, ldk, (const T*)V, ldv, H, D, b, rope, n_pos, \
+                                                                        eps, (unsigned char*)pages)
+#define KP_LPT(T, VEC)                      \
+  do {                                      \
+    if (D <= 64) KP_GO(T, 8, VEC);          \
+    else if (D <= 128) KP_GO(T, 16, VEC);   \
+    else KP_GO(T, 32, VEC);                 \
+  } while (0)
+  if (dt == BL_BF16) { if (vec) KP_LPT(uint16_t, true); else KP_LPT(uint16_t, false); }
+  else { if (vec) KP_LPT(u32, true); else KP_LPT(u32, false); }
+#undef KP_LPT
+#undef KP_GO
+  BL_HIP_CHECK_LAUNCH();
+  return BL_OK;
+}
+
+// ---------------------------------------------------------------- reading the codes back
+// value = level * scale, one float32 multiply (bfloat16 outputs: one rounding more).
+__device__ __forceinline__ float kp_level(u32 mag, u32 neg, u32 low, bool four) {
+  const float m = (float)(four ? 2 * mag + low : mag);
+  return neg ? -m : m;
+}
+template <typename OutT>
+__device__ __forceinline__ void kp_store2(OutT* p, float x, float y) {
+  if (sizeof(OutT) == 2) *reinterpret_cast<u32*>(p) = (u32)bl_f32_to_bf16_rne(x) | ((u32)bl_f32_to_bf16_rne(y) << 16);
+  else *reinterpret_cast<float2*>(p) = make_float2(x, y);
+}
+
+template <typename OutT>
+__global__ __launch_bounds__(KP_THREADS) void kv_read_kernel(const unsigned char* __restrict__ pages, int H, int D, KvBatch b,
+                                                             OutT* __restrict__ K, OutT* __restrict__ V) {
+  const int h = (int)(blockIdx.x % (unsigned)H);
+  KvSeq q;
+  const int64_t local = kp_find(b, blockIdx.x / (unsigned)H, 1, 7, 2, q);
+  if (local < 0) return;
+  const int64_t pg = (q.pos0 > 0 ? q.pos0 >> 7 : 0) + local;
+  if (pg >= b.max_pages || pg * KP_TOKENS >= q.len) return;
+  const int id = b.table[(int64_t)q.s * b.max_pages + pg];
+  if (id < 0 || id >= b.n_pages) return;
+  const int a = (int)max(q.pos0 - pg * KP_TOKENS, (int64_t)0), e = (int)min(q.len - pg * KP_TOKENS, (int64_t)KP_TOKENS);
+  const int U = kp_units(D);
+  const unsigned char* head = pages + ((int64_t)id * H + h) * kp_head_bytes(U);
+  const float* k_scale = reinterpret_cast<const float*>(head + kp_scale_off(U));
+  const float* v_scale = k_scale + KP_TOKENS;
+  const u32* lows = reinterpret_cast<const u32*>(head + kp_low_off(U));
+  const int64_t row0 = q.q0 + pg * KP_TOKENS - q.pos0;      // row of the page's token 0
+  if (K) {
+    // a thread: 8 channels of one token
+    const u32* words = reinterpret_cast<const u32*>(head);
+    for (int it = threadIdx.x; it < (e - a) * 4 * U; it += KP_THREADS) {
+      const int tok = a + it / (4 * U), o8 = it % (4 * U), u = o8 >> 2, k = o8 & 3;
+      const u32* w = words + (kp_slot(tok) * U + u) * 3;
+      const bool four = pg == 0 && tok == 0;
+      const u32 m = w[k >> 1] >> (2 * (k & 1)), sg = w[2] >> (3 - k), lo = four ? lows[u] >> (3 - k) : 0u;
+      const float d = k_scale[tok];
+      OutT* out = K + ((row0 + tok) * H + h) * (int64_t)D;
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const int c = 8 * o8 + i;
+        if (c < D)                                         // (D is even)
+          kp_store2<OutT>(out + c, kp_level((m >> (4 * i)) & 3u, (sg >> (4 * i)) & 1u, (lo >> (4 * i)) & 1u, four) * d,
+                          kp_level((m >> (4 * i + 4)) & 3u, (sg >> (4 * i + 4)) & 1u, (lo >> (4 * i + 4)) & 1u, four) * d);
+      }
+    }
+  }
+  if (V) {
+    // a thread: two channels of 32 tokens
+    const u32* words = reinterpret_cast<const u32*>(head + kp_code_bytes(U));
+    const int pairs = D >> 1;
+    for (int it = threadIdx.x; it < 4 * pairs; it += KP_THREADS) {
+      const int g = it / pairs, d = 2 * (it - g * pairs);
+      const int lo = max(a - 32 * g, 0), hi = min(e - 32 * g, 32);
+      if (lo >= hi) continue;
+      u32 w[2][3];
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) w[p][k] = words[((d + p) * 4 + g) * 3 + k];
+      u32 low[2] = {0u, 0u};
+      if (pg == 0 && g == 0) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) low[p] = (lows[U + ((d + p) >> 5)] >> kp_sign_bit((d + p) & 31)) & 1u;
+      }
+      OutT* out = V + ((row0 + 32 * g) * H + h) * (int64_t)D + d;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        if (i < lo || i >= hi) continue;
+        const bool four = pg == 0 && g == 0 && i == 0;
+        const float sc = v_scale[32 * g + i];
+        float x[2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) x[p] = kp_level((w[p][i >> 4] >> kp_mag_bit(i)) & 3u, (w[p][2] >> kp_sign_bit(i)) & 1u, low[p], four) * sc;
+        kp_store2<OutT>(out + (int64_t)i * H * D, x[0], x[1]);
+      }
+    }
+  }
+}
+
+int bl_launch_kv_read(const void* pages, int H, int D, const KvBatch& b, void* K, void* V, bl_dtype odt, hipStream_t s) {
+  const int64_t blocks = kp_items(b.T, b.n_seqs) * H;
+  if (!bl_grid_ok(blocks)) return BL_ESHAPE;
+  if (odt == BL_BF16) kv_read_kernel<uint16_t><<<(unsigned)blocks, KP_THREADS, 0, s>>>((const unsigned char*)pages, H, D, b, (uint16_t*)K, (uint16_t*)V);
+  else kv_read_kernel<float><<<(unsigned)blocks, KP_THREADS, 0, s>>>((const unsigned char*)pages, H, D, b, (float*)K, (float*)V);
+  BL_HIP_CHECK_LAUNCH();
+  return BL_OK;
+}
