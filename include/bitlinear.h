@@ -374,17 +374,18 @@ int kv_cache_read(const void* cache, const float* scales, int64_t pos0, int64_t 
  *   rope       nullable; device, float32 [n_pos, D], n_pos >= 128 max_pages: per position the cosines for channel pairs (i, i + D / 2),
  *              i < D / 2, then their sines.  Keys and queries are rotated on the way in: x_i c - x_(i+D/2) s, x_(i+D/2) c + x_i s.
  *   D          even, 2 ... 256
- * kv_pages_append: K, V device [T, H, D] of x_dtype, row t at element t * ldk, t * ldv (ldk, ldv >= H * D, heads dense), 16-byte
- *   aligned bases.  Float32 steps as in quantize_heads; rows are written whatever order sequences and pages stand in.
+ * kv_pages_append: K, V device [T, H, D] of x_dtype, row t at element t * ldk, t * ldv (ldk, ldv >= H * D, heads dense; slices of a
+ *   fused product's output).  Bases need their elements' alignment only; 16-byte aligned rows with D % 16 == 0 are faster.  Float32 steps as
+ *   in quantize_heads; rows are written whatever order sequences and pages stand in.
  * kv_pages_read: the values of the batch's rows, K_out, V_out [T, H, D] of out_dtype, dense (either may be NULL).  (With q_start the
  *   running sums of kv_len it reads whole sequences.)
  * kv_pages_attention: O[t] = sum_j p_j v_j / sum_j p_j over the visible positions j of the row's sequence, p_j = exp(scale * q . k_j)
  *   relative to the largest; position j is visible to a row at position i if j <= i, and, where window > 0, j > i - window or
  *   j < sinks.  A row that sees nothing (or only absent pages) gives zeros.
- *   Q          device [T, Hq, D] of q_dtype, row t at element t * ldq, 16-byte aligned; Hq a multiple of H: query head h reads head
+ *   Q          device [T, Hq, D] of q_dtype, row t at element t * ldq, aligned to its elements; Hq a multiple of H: query head h reads head
  *              h / (Hq / H)
- *   q_bits     16: queries as they are (kept to 8 significand bits, so bfloat16 ones exactly); 4: quantize_heads' 4-bit levels of the
- *              rotated query (Table 3's 4-bit Q), eps its epsilon
+ *   q_bits     16: queries as they are (rotated, every channel kept to 1 / 7680 of the row's largest); 4: quantize_heads' 4-bit levels of
+ *              the rotated query (Table 3's 4-bit Q), eps its epsilon
  *   O          device, bfloat16 [T, Hq, D], dense, 16-byte aligned
  *   workspace  kv_pages_attention_workspace_bytes(T, n_seqs, Hq, H, D, max_pages) bytes, 16-byte aligned (may be 0: then NULL); what a
  *              call leaves there means nothing to the next, but calls that may overlap in time need one each

@@ -149,11 +149,11 @@ def cached(pool, table, s, h, values):
 # ---------------------------------------------------------------- attention
 def attention(Q, pool, table, q_start, kv_len, rope, scale, window=0, sinks=0, q_bits=16, eps=O.DEFAULT_EPS):
     """float64 outputs [T, Hq, D] (NaN in rows of no sequence), and what a tolerance needs: sum p |v| / sum p [T, Hq, D], the largest
-    scale * sum |q| |k| over visible keys [T, Hq], largest value scale over sum p [T, Hq], visible keys [T, Hq]."""
+    scale * sum |q| |k| and scale * max |q| * sum |k| over visible keys [T, Hq, 2], largest |v| over sum p [T, Hq], visible keys [T, Hq]."""
     T, Hq, D = Q.shape
     G = Hq // pool.H
     o, a = np.full((T, Hq, D), np.nan), np.zeros((T, Hq, D))
-    mass, unit, seen_n = np.zeros((T, Hq)), np.zeros((T, Hq)), np.zeros((T, Hq), int)
+    mass, unit, seen_n = np.zeros((T, Hq, 2)), np.zeros((T, Hq)), np.zeros((T, Hq), int)
     for s in range(len(kv_len)):
         r0, pos = rows_of(q_start, kv_len, s)
         if not len(pos):
@@ -181,7 +181,8 @@ def attention(Q, pool, table, q_start, kv_len, rope, scale, window=0, sinks=0, q
                 l = np.where(see.any(1), p.sum(1), 1)
                 at = slice(r0, r0 + len(pos))
                 o[at, g], a[at, g] = (p @ v) / l[:, None], (p @ np.abs(v)) / l[:, None]
-                mass[at, g] = np.where(see, scale * (np.abs(q[:, g]) @ np.abs(k).T), 0).max(1)
+                mass[at, g, 0] = np.where(see, scale * (np.abs(q[:, g]) @ np.abs(k).T), 0).max(1)
+                mass[at, g, 1] = np.where(see, scale * np.abs(q[:, g]).max(1, keepdims=True) * np.abs(k).sum(1), 0).max(1)
                 unit[at, g] = np.abs(v).max() / l
                 seen_n[at, g] = see.sum(1)
     return o, a, mass, unit, seen_n

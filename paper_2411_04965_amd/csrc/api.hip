@@ -268,7 +268,8 @@ static KvBatch kv_batch(const int32_t* q_start, const int32_t* kv_len, int64_t n
                         int64_t n_pages, int64_t T) {
   return KvBatch{q_start, kv_len, table, (int)n_seqs, (int)max_pages, (int)n_pages, (int)T};
 }
-// rows of `heads` dense heads, a stride apart
+// rows of `heads` dense heads, a stride apart, may start at any element (a slice of a fused product's output)
+static bool aligned_elems(const void* p, bl_dtype dt) { return (reinterpret_cast<uintptr_t>(p) & (dt == BL_F32 ? 3 : 1)) == 0; }
 static bool kv_rows_ok(int64_t T, int64_t heads, int64_t D, int64_t ld) {
   return ld >= heads * D && ld <= ((int64_t)1 << 40) / T;
 }
@@ -281,7 +282,7 @@ extern "C" int kv_pages_append(const void* K, int64_t ldk, const void* V, int64_
   int rc = kv_pages_check(T, H, D, q_start, kv_len, n_seqs, page_table, max_pages, rope, n_pos, pages, n_pages);
   if (rc) return rc;
   if (!kv_rows_ok(T, H, D, ldk) || !kv_rows_ok(T, H, D, ldv)) return BL_EINVAL;
-  if (!bl_aligned16(K) || !bl_aligned16(V)) return BL_EALIGN;
+  if (!aligned_elems(K, x_dtype) || !aligned_elems(V, x_dtype)) return BL_EALIGN;
   return bl_launch_kv_append(K, ldk, V, ldv, x_dtype, (int)H, (int)D, kv_batch(q_start, kv_len, n_seqs, page_table, max_pages, n_pages, T),
                              rope, n_pos, eps, pages, (hipStream_t)stream);
 }
@@ -317,7 +318,7 @@ extern "C" int kv_pages_attention(const void* Q, int64_t ldq, bl_dtype q_dtype, 
   if (Hq < H || Hq % H != 0) return BL_EINVAL;
   if (Hq > (1 << 20) || T > (((int64_t)1 << 31) - 1) / (Hq / H)) return BL_ESHAPE;
   if (!kv_rows_ok(T, Hq, D, ldq)) return BL_EINVAL;
-  if (!bl_aligned16(Q) || !bl_aligned16(O)) return BL_EALIGN;
+  if (!aligned_elems(Q, q_dtype) || !bl_aligned16(O)) return BL_EALIGN;
   const size_t need = bl_kv_attention_ws_bytes(T, n_seqs, Hq / H, H, D, max_pages);
   if (need && (!workspace || workspace_bytes < need)) return BL_EWORKSPACE;
   if (need && !bl_aligned16(workspace)) return BL_EALIGN;

@@ -44,7 +44,7 @@ def test_shared_refusals(L, call, bad, status):
 
 @pytest.mark.parametrize("bad,status", [
     (dict(K=None), -1), (dict(V=None), -1), (dict(eps=-1.0), -1), (dict(eps=float("nan")), -1), (dict(ldk=255), -1), (dict(ldv=0), -1),
-    (dict(ldk=-256), -1), (dict(ldv=1 << 50), -1), (dict(K=P + 8), -3), (dict(V=P + 2), -3), (dict(rope=P, n_pos=255), -2),
+    (dict(ldk=-256), -1), (dict(ldv=1 << 50), -1), (dict(K=P + 1), -3), (dict(V=P + 2, dt=0), -3), (dict(rope=P, n_pos=255), -2),
     (dict(rope=P + 2, n_pos=256), -3)])
 def test_append_refusals(L, bad, status):
     assert append(L, **bad) == status
@@ -58,7 +58,7 @@ def test_read_refusals(L, bad, status):
 @pytest.mark.parametrize("bad,status", [
     (dict(Q=None), -1), (dict(O=None), -1), (dict(bits=8), -1), (dict(bits=3), -1), (dict(eps=-1.0), -1), (dict(scale=0.0), -1),
     (dict(scale=-0.1), -1), (dict(scale=INF), -1), (dict(scale=float("nan")), -1), (dict(window=-1), -1), (dict(sinks=-1), -1),
-    (dict(Hq=3), -1), (dict(Hq=0), -1), (dict(ldq=511), -1), (dict(ldq=1 << 50), -1), (dict(Q=P + 8), -3), (dict(O=P + 2), -3),
+    (dict(Hq=3), -1), (dict(Hq=0), -1), (dict(ldq=511), -1), (dict(ldq=1 << 50), -1), (dict(Q=P + 1), -3), (dict(Q=P + 2, dt=0), -3), (dict(O=P + 2), -3),
     (dict(rope=P, n_pos=255), -2), (dict(T=(1 << 30) - 1, Hq=8, ldq=1024), -2),
     (dict(mp=64, ws=None), -4), (dict(mp=64, wsb=64), -4), (dict(mp=64, ws=P + 8), -3)])
 def test_attention_refusals(L, bad, status):

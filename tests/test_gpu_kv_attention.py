@@ -11,13 +11,14 @@ from tests.gpu_util import dev, host
 pytestmark = pytest.mark.gpu
 
 
-def tolerance(o, a, mass, unit, n, D, q_rounded):
-    """A score loses at most (D + 8) 2^-24 of sum |q| |k| in float32, and 2^-8 of it where the query is rounded to two E4M3 parts (2^-4
-    of 2^-4; float32 and rotated queries; below 2^-22 of the row's largest channel the parts end, which adds 2^-14).  That shifts every
-    term by a factor exp(x), numerator and denominator alike: 2 (exp(x) - 1) of sum p |v| / sum p.  A term is rounded to 8 significand
-    bits (2^-8; the parts end at 2^-22 of the largest value scale: 3 levels, n terms), exp2, the float32 sums and their rescalings take
-    2^-16 more; the output its bfloat16 rounding 2^-8."""
-    x = mass * ((D + 8) * 2.0 ** -24 + ((2.0 ** -8 + 2.0 ** -14) if q_rounded else 0.0))
+def tolerance(o, a, mass, unit, n, D, q_bits):
+    """A score loses at most (D + 8) 2^-24 of sum |q| |k| in float32.  A query that is not quantized is kept in steps of 1 / 3840 of its
+    largest channel (largest = 15, three digits of a sixteenth each): every channel is off by half a step, the score by that times
+    sum |k|, and by 2^-22 of sum |q| |k| for the two roundings of the division and the product.  That shifts every term by a factor
+    exp(x), numerator and denominator alike: 2 (exp(x) - 1) of sum p |v| / sum p.  A term is rounded to 8 significand bits (2^-8; the
+    parts end at 2^-22 of the largest value scale: 3 levels, n terms), exp2, the float32 sums and their rescalings take 2^-16 more;
+    the output its bfloat16 rounding 2^-8."""
+    x = mass[..., 0] * ((D + 8) * 2.0 ** -24 + 2.0 ** -22) + (mass[..., 1] / 7680 if q_bits == 16 else 0.0)
     e = (2 * np.expm1(x)[..., None] + 2.0 ** -8 + 2.0 ** -16) * a + n[..., None] * 2.0 ** -22 * 2 * unit[..., None]
     return e + 2.0 ** -8 * (np.abs(o) + e) + 1e-30
 
@@ -43,7 +44,7 @@ def run(b, Hq, q_dtype=BF16, rope=False, window=0, sinks=0, q_bits=16, scale=Non
     got, o, a, mass, unit, n = (t[:rows] for t in (got, o, a, mass, unit, n))
     assert np.isfinite(got).all()
     assert (got[n == 0] == 0).all(), "rows that see nothing"
-    tol = tolerance(o, a, mass, unit, n, b.D, q_bits == 16 and (rope or q_dtype == F32))
+    tol = tolerance(o, a, mass, unit, n, b.D, q_bits)
     err = np.abs(got - o)
     assert (err <= tol).all(), "err / tol %.3g at %s" % ((err / tol).max(), np.argwhere(err > tol)[:4].tolist())
     return out
