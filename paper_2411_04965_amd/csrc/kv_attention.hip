@@ -24,6 +24,7 @@
 
 #define KA_THREADS 256
 #define KA_WAVES 4
+#define KA_QT(DT) ((DT) == 256 ? 1 : 2)      // tiles of 16 rows a wave where the rows fill the chip
 
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef short v2s __attribute__((ext_vector_type(2)));
@@ -31,7 +32,7 @@ typedef short v2s __attribute__((ext_vector_type(2)));
 struct KaArgs {
   const void* Q;
   int64_t ldq, n_pos;
-  int q_f32, q_vec, Hq, H, G, D;          // H: key / value heads, G = Hq / H query heads each
+  int q_f32, Hq, H, G, D;          // H: key / value heads, G = Hq / H query heads each
   KvBatch b;
   const float* rope;
   float cs, eps;                          // cs = scale * log2(e)
@@ -53,15 +54,21 @@ __device__ __forceinline__ v4f ka_mfma_qk(const u32 (&a)[4], const u32 (&b)[6], 
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, c, 4 /* rows: E2M1 */, 2 /* columns: E2M3 */, 0, sa, 0, sb);
 }
 
-// Four floats below 2^8 as hi + 2^-5 lo, both E4M3
-__device__ __forceinline__ void ka_split4(const float (&x)[4], int& hi, int& lo) {
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+// Four floats below 2^8 as hi + 2^-5 lo, both E4M3.  `old`: any value (the conversions write a half each).
+__device__ __forceinline__ void ka_split4(const float (&x)[4], int old, int& hi, int& lo) {
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], old, false);
   hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], hi, true);
-  const v2f b0 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), b1 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32((x[0] - b0.x) * 32.0f, (x[1] - b0.y) * 32.0f, 0, false);
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32((x[2] - b1.x) * 32.0f, (x[3] - b1.y) * 32.0f, lo, true);
+  const v2f b0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, 32.0f, false), b1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, 32.0f, true);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_fmaf(x[0], 32.0f, -b0.x), __builtin_fmaf(x[1], 32.0f, -b0.y), hi, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_fmaf(x[2], 32.0f, -b1.x), __builtin_fmaf(x[3], 32.0f, -b1.y), lo, true);
 }
 
+// (fmaxf would first make each argument canonical: twice the instructions over scores that come out of a select)
+__device__ __forceinline__ float ka_max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 __device__ __forceinline__ float ka_max_groups(float v) {      // over the four lanes of a query
   v = fmaxf(v, __shfl_xor(v, 16, 64));
   return fmaxf(v, __shfl_xor(v, 32, 64));
@@ -70,45 +77,28 @@ __device__ __forceinline__ float ka_max_groups(float v) {      // over the four 
 __device__ __forceinline__ float ka_q_at(const KaArgs& p, int64_t at) {
   return p.q_f32 ? reinterpret_cast<const float*>(p.Q)[at] : bl_bf16_to_f32(reinterpret_cast<const uint16_t*>(p.Q)[at]);
 }
-
-// 16 channels from c on of the head that starts at element `at`
-__device__ __forceinline__ void ka_load16(const KaArgs& p, int64_t at, int c, float (&x)[16]) {
-  if (p.q_vec) {
-    if (c >= p.D) {
+// 16 bfloat16 channels at a 16-byte boundary
+__device__ __forceinline__ void ka_bf16x16(const uint4 (&w)[2], float (&x)[16]) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = 0.0f;
-    } else if (p.q_f32) {
-      const float4* s = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.Q) + at + c);
+  for (int e = 0; e < 2; ++e) {
+    const u32 ww[4] = {w[e].x, w[e].y, w[e].z, w[e].w};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float4 w = s[e];
-        x[4 * e] = w.x; x[4 * e + 1] = w.y; x[4 * e + 2] = w.z; x[4 * e + 3] = w.w;
-      }
-    } else {
-      const uint4* s = reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p.Q) + at + c);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint4 w = s[e];
-        const u32 ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[8 * e + 2 * i] = __uint_as_float(ww[i] << 16);
-          x[8 * e + 2 * i + 1] = __uint_as_float(ww[i] & 0xFFFF0000u);
-        }
-      }
+    for (int i = 0; i < 4; ++i) {
+      x[8 * e + 2 * i] = __uint_as_float(ww[i] << 16);
+      x[8 * e + 2 * i + 1] = __uint_as_float(ww[i] & 0xFFFF0000u);
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] = c + e < p.D ? ka_q_at(p, at + c + e) : 0.0f;
   }
 }
 
 // One query's operands: lane group g holds the digits of channels 32 g .. 32 g + 31 of every 128.  DT = 64: the second half of the
 // contraction takes the second digit against the same codes, so two instructions do.
-template <int DT, bool Q4>
+// QV: bfloat16 rows at 16-byte boundaries with D % 32 == 0 (16 channels then lie in one half of the rotation's pairs): all loads of a
+// row go out together.  Other rows go channel by channel.
+template <int DT, bool Q4, bool QV>
 struct KaQuery {
   static constexpr int KS = DT == 256 ? 2 : 1;
   static constexpr int PARTS = Q4 ? 1 : DT == 64 ? 2 : 3;
+  static constexpr int WORDS = KS * PARTS * 6;
   u32 op[KS][PARTS][6];
   float c;                                 // log2 units of a score that is product * key scale
   int pos;                                 // position; -1: no such row
@@ -128,39 +118,79 @@ struct KaQuery {
     float x[KS][2][16];
     const int half = p.D >> 1;
     const float* rr = p.rope ? p.rope + min(max(ps, (int64_t)0), p.n_pos - 1) * p.D : nullptr;
-    float top = 0.0f;
+    if (QV) {
+      const uint16_t* row = reinterpret_cast<const uint16_t*>(p.Q) + at;
+      uint4 w[KS][2][2], o[KS][2][2];
+      float4 cs[KS][2][4], sn[KS][2][4];
 #pragma unroll
-    for (int k = 0; k < KS; ++k)
+      for (int k = 0; k < KS; ++k)
 #pragma unroll
-      for (int v = 0; v < 2; ++v) {
-        const int ch = 128 * k + 32 * (DT == 64 ? g & 1 : g) + 16 * v;
-        float (&y)[16] = x[k][v];
-        ka_load16(p, at, ch, y);
-        if (rr) {
-          if (p.q_vec) {                            // D % 32 == 0: 16 channels lie in one half
-            if (ch < p.D) {
-              float o[16];
-              ka_load16(p, at, ch < half ? ch + half : ch - half, o);
+        for (int v = 0; v < 2; ++v) {
+          const int ch = min(128 * k + 32 * (DT == 64 ? g & 1 : g) + 16 * v, p.D - 16);
+          const int other = ch < half ? ch + half : ch - half, pair = ch < half ? ch : ch - half;
 #pragma unroll
-              for (int e = 0; e < 16; ++e) y[e] = kp_rotate(y[e], o[e], rr, ch + e, half);
-            }
-          } else {
+          for (int e = 0; e < 2; ++e) w[k][v][e] = reinterpret_cast<const uint4*>(row + ch)[e];
+          if (rr) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int cc = ch + e;
-              if (cc < p.D) y[e] = kp_rotate(y[e], ka_q_at(p, at + (cc < half ? cc + half : cc - half)), rr, cc, half);
+            for (int e = 0; e < 2; ++e) o[k][v][e] = reinterpret_cast<const uint4*>(row + other)[e];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              cs[k][v][e] = reinterpret_cast<const float4*>(rr + pair)[e];
+              sn[k][v][e] = reinterpret_cast<const float4*>(rr + half + pair)[e];
             }
           }
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          if (!have) y[e] = 0.0f;
-          top = fmaxf(top, fabsf(y[e]));
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const int ch = 128 * k + 32 * (DT == 64 ? g & 1 : g) + 16 * v;
+          float (&y)[16] = x[k][v];
+          ka_bf16x16(w[k][v], y);
+          if (rr) {                        // kp_rotate's steps; the first half subtracts
+            float t[16];
+            ka_bf16x16(o[k][v], t);
+            const u32 flip = ch < half ? 0x80000000u : 0u;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float4 c4 = cs[k][v][e >> 2], s4 = sn[k][v][e >> 2];
+              const float cc = (e & 3) == 0 ? c4.x : (e & 3) == 1 ? c4.y : (e & 3) == 2 ? c4.z : c4.w;
+              const float ss = (e & 3) == 0 ? s4.x : (e & 3) == 1 ? s4.y : (e & 3) == 2 ? s4.z : s4.w;
+              y[e] = y[e] * cc + __uint_as_float(__float_as_uint(t[e]) ^ flip) * ss;
+            }
+          }
+          if (ch >= p.D) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) y[e] = 0.0f;
+          }
         }
-      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int ch = 128 * k + 32 * (DT == 64 ? g & 1 : g) + 16 * v + e;
+            float y = 0.0f;
+            if (ch < p.D) {
+              y = ka_q_at(p, at + ch);
+              if (rr) y = kp_rotate(y, ka_q_at(p, at + (ch < half ? ch + half : ch - half)), rr, ch, half);
+            }
+            x[k][v][e] = y;
+          }
+    }
+    float top = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int v = 0; v < 2; ++v)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[k][v][e]));
     top = ka_max_groups(top);
     const float lv = Q4 ? 7.0f : 15.0f;
-    const float f = Q4 ? 7.0f / (top + p.eps) : top > 0.0f ? 15.0f / top : 0.0f;
+    float f = Q4 ? 7.0f / (top + p.eps) : top > 0.0f ? 15.0f / top : 0.0f;
+    if (!have) f = 0.0f;
     c = fmaxf(16.0f * p.cs * (top / lv), 1.17549435e-38f);      // digits are eighths, codes halves; never 0 (times -inf)
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
@@ -170,19 +200,17 @@ struct KaQuery {
         for (int e = 0; e < 6; ++e) op[k][w][e] = 0;
 #pragma unroll
       for (int e = 0; e < 32; ++e) {
+        // magnitude in 256ths of a unit: the digits are its three nibbles, the sign is theirs alike
         const float y = x[k][e >> 4][e & 15] * f;
-        float d[3];
-        d[0] = fminf(fmaxf(rintf(y), -lv), lv);
-        const float r1 = (y - d[0]) * 16.0f;
-        d[1] = fminf(fmaxf(rintf(r1), -15.0f), 15.0f);
-        d[2] = fminf(fmaxf(rintf((r1 - d[1]) * 16.0f), -15.0f), 15.0f);
-        if (DT == 64 && !Q4) {
-          if (g >= 2) { d[0] = d[1]; d[1] = 0.0f; } else d[1] = d[2];
+        const u32 sg = (__float_as_uint(y) >> 26) & 32u;
+        const u32 m = Q4 ? (u32)fminf(rintf(fabsf(y)), 7.0f) << 8 : (u32)fminf(rintf(fabsf(y) * 256.0f), 3840.0f);
+        u32 d[3] = {m >> 8, (m >> 4) & 15u, m & 15u};
+        if (DT == 64) {
+          if (g >= 2) { d[0] = Q4 ? 0u : d[1]; d[1] = 0u; } else d[1] = d[2];
         }
-        if (DT == 64 && Q4 && g >= 2) d[0] = 0.0f;
 #pragma unroll
         for (int w = 0; w < PARTS; ++w) {
-          const u32 code = (u32)fabsf(d[w]) | (d[w] < 0.0f ? 32u : 0u);
+          const u32 code = d[w] | sg;
           const int bit = 6 * e;
           op[k][w][bit >> 5] |= code << (bit & 31);
           if ((bit & 31) > 26) op[k][w][(bit >> 5) + 1] |= code >> (32 - (bit & 31));
@@ -267,34 +295,104 @@ __device__ __forceinline__ void ka_load_scales(const float* s, float (&v)[8][4])
   }
 }
 
-// probabilities of 16 queries as the second product's operands; MASKED: what is not seen has no weight, whatever stands there
-template <bool MASKED>
-__device__ __forceinline__ void ka_weights(const v4f (&S)[8], const float (&vs)[8][4], float c, float base, float& l, v8i& ph, v8i& pl) {
+// a * b, and 0 where either is 0, whatever the other is (the instruction, so that the compiler knows of it)
+extern "C" __device__ float ka_mul_legacy(float a, float b) __asm("llvm.amdgcn.fmul.legacy");
+
+// Probabilities of 16 queries as the second product's operands; scales(t): the four value scales of scores t.  What is not seen has
+// probability 0, and 0 times a scale that is infinite or no number is 0 here.
+template <typename F>
+__device__ __forceinline__ void ka_weights(const v4f (&S)[8], F scales, float c, float base, float& l, v8i& ph, v8i& pl) {
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int t = 0; t < 8; ++t) {
+    const float4 s4 = scales(t);
+    const float vs[4] = {s4.x, s4.y, s4.z, s4.w};
     float w[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t][r], c, -base));
       sum[r] += e;
-      w[r] = e * vs[t][r];
-      if (MASKED && e == 0.0f) w[r] = 0.0f;
+      w[r] = ka_mul_legacy(e, vs[r]);
     }
     int hi, lo;
-    ka_split4(w, hi, lo);
+    ka_split4(w, __float_as_int(S[t][0]), hi, lo);
     ph[t] = hi;
     pl[t] = lo;
   }
   l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
+// a scale as far as it counts for E: one that is infinite or no number may belong to a place that some rows do not see
+__device__ __forceinline__ float ka_finite(float s) { return __float_as_uint(s) < 0x7F800000u ? s : 0.0f; }
+// E of a largest value scale: scales times ka_scale_factor(E) = 2^(134 - E) are below 2^8, E - 7 is the E8M0 of what that took away
+__device__ __forceinline__ int ka_exponent(float top) { return min(max((int)(__float_as_uint(top) >> 23), 16), 254); }
+__device__ __forceinline__ float ka_scale_factor(int E) { return __uint_as_float((u32)(261 - E) << 23); }
 
-// One page against QT x 16 queries.  keys: the page's; on return those of `next` (nullptr: none) are on their way.
-template <int DT, int QT, bool Q4>
+// Operands of the first token's lowest magnitude bits (nibble 1 = half a level, of the sign in C): 32 channels of the key ...
+__device__ __forceinline__ void ka_low_keys(u32 low, u32 C, u32 (&a)[4]) {
+#pragma unroll
+  for (int v = 0; v < 4; ++v) a[v] = (((low << v) & 0x88888888u) >> 3) | ((C << v) & 0x88888888u);
+}
+// ... and, of the values of channels 16 d ..., token 0 alone
+__device__ __forceinline__ void ka_low_values(const u32* lows, int U, int d, u32 C, u32 (&a)[4]) {
+  const int lane = threadIdx.x & 63, c0 = min(16 * d, 32 * U - 16);
+  const u32 bit = (lows[U + (c0 >> 5)] >> kp_sign_bit((c0 & 16) + (lane & 15))) & 1u;
+  a[0] = lane < 16 ? bit | (C & 8u) : 0u;
+  a[1] = a[2] = a[3] = 0u;
+}
+
+// Scores of 16 queries against a page, masked where some are not seen; `hi` and so on are a row's own.
+__device__ __forceinline__ bool ka_masked(const KaArgs& p, const KaRange& rg, int64_t t0) {
+  return t0 + KP_TOKENS - 1 > rg.min_pos || (p.window && t0 <= rg.max_pos - p.window && t0 + KP_TOKENS > p.sinks);
+}
+// Places of the page that rows from position `first` to `last` see: lo + 1 .. hi, and those below snk, less 16 g
+struct KaSeen {
+  int hi, lo, snk;
+  __device__ __forceinline__ KaSeen(const KaArgs& p, int64_t t0, int64_t first, int64_t last, int base) {
+    auto clamp = [&](int64_t v) { return (int)min(max(v - t0, (int64_t)-1), (int64_t)KP_TOKENS); };
+    hi = clamp(last) - base;
+    lo = (p.window ? clamp(first - p.window) : -1) - base;
+    snk = (int)min(max((int64_t)p.sinks - t0, (int64_t)0), (int64_t)KP_TOKENS) - base;
+  }
+  __device__ __forceinline__ bool at(int j) const { return j <= hi && (j > lo || j < snk); }
+};
+// lane group g, scores t, element r: token 64 (t / 4) + 16 g + 4 (t % 4) + r of the page
+__device__ __forceinline__ constexpr int ka_token(int t, int r) { return 64 * (t >> 2) + 4 * (t & 3) + r; }
+
+__device__ __forceinline__ void ka_mask(v4f (&S)[8], KaSeen see) {
+  // (without a window most comparisons are the same for every page: kept here, not held in registers over the loop)
+  asm volatile("" : "+v"(see.hi), "+v"(see.lo), "+v"(see.snk));
+#pragma unroll
+  for (int t = 0; t < 8; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) S[t][r] = see.at(ka_token(t, r)) ? S[t][r] : -INFINITY;
+}
+
+// New maximum over a page's scores, what was summed so far brought to it; -> the maximum in log2 units
+template <int DT>
+__device__ __forceinline__ float ka_rescale(const v4f (&S)[8], float c, KaState<DT>& st) {
+  float mx = -INFINITY;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) mx = ka_max3(ka_max3(mx, S[t][0], S[t][1]), S[t][2], S[t][3]);
+  const float m = fmaxf(st.m, ka_max_groups(mx));
+  const float base = m == -INFINITY ? 0.0f : m * c;      // nothing seen so far: all terms are exp2(-inf) = 0
+  if (__any(m > st.m)) {
+    const float al = __builtin_amdgcn_exp2f(st.m * c - base);
+    st.l *= al;
+#pragma unroll
+    for (int t = 0; t < DT / 16; ++t) st.o[t] *= al;
+    st.m = m;
+  }
+  return base;
+}
+
+// One page against 16 queries.  keys: the page's key codes; on return those of `next` (nullptr: none) are on their way.  Values and
+// scales are fetched with the scores' products ahead of them.
+// FIRST: the sequence's page 0.
+template <bool FIRST, int DT, bool Q4, bool QV>
 __device__ __forceinline__ void ka_page(const KaArgs& p, const KaRange& rg, int page, const unsigned char* head,
                                         const unsigned char* next, int U, KaCodes<DT == 256 ? 16 : 8>& keys,
-                                        const KaQuery<DT, Q4> (&qy)[QT], KaState<DT> (&st)[QT]) {
-  typedef KaQuery<DT, Q4> Query;
+                                        const KaQuery<DT, Q4, QV>& qy, KaState<DT>& st) {
+  typedef KaQuery<DT, Q4, QV> Query;
   constexpr int KS = Query::KS, PARTS = Query::PARTS;
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const float* k_scale = reinterpret_cast<const float*>(head + kp_scale_off(U));
@@ -305,128 +403,86 @@ __device__ __forceinline__ void ka_page(const KaArgs& p, const KaRange& rg, int 
   ka_load_values<DT>(head, U, vals);
   ka_load_scales(k_scale + KP_TOKENS, vs);
 
-  // scores: S[i][t] = codes of 16 tokens x queries
-  v4f S[QT][8];
+  v4f S[8];
 #pragma unroll
   for (int t = 0; t < 8; ++t) {
-#pragma unroll
-    for (int i = 0; i < QT; ++i) S[i][t] = (v4f){0.f, 0.f, 0.f, 0.f};
+    S[t] = (v4f){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       u32 a[4];
       const auto w = keys.w[t * KS + k];
       kp_expand(w.a, w.b, w.c, a);
 #pragma unroll
-      for (int i = 0; i < QT; ++i)
-#pragma unroll
-        for (int d = 0; d < PARTS; ++d) S[i][t] = ka_mfma_qk(a, qy[i].op[k][d], S[i][t], 127, Query::scale(d, g));
+      for (int d = 0; d < PARTS; ++d) S[t] = ka_mfma_qk(a, qy.op[k][d], S[t], 127, Query::scale(d, g));
     }
   }
-  if (page == 0) {                         // the first token's lowest bits
-    ks[0][0] *= g == 0 ? 2.0f : 1.0f;
-    vs[0][0] *= g == 0 ? 2.0f : 1.0f;
+  if (FIRST) {                             // the first token's lowest bits
+    if (g == 0) { ks[0][0] *= 2.0f; vs[0][0] *= 2.0f; }
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
-      const u32 L = n == 0 ? lows[min(DT == 64 ? g & 1 : 4 * k + g, U - 1)] : 0u, C = keys.w[k].c;
+      const u32 L = n == 0 ? lows[min(DT == 64 ? g & 1 : 4 * k + g, U - 1)] : 0u;
       u32 a[4];
+      ka_low_keys(L, keys.w[k].c, a);
 #pragma unroll
-      for (int v = 0; v < 4; ++v) a[v] = (((L << v) & 0x88888888u) >> 3) | ((C << v) & 0x88888888u);
-#pragma unroll
-      for (int i = 0; i < QT; ++i)
-#pragma unroll
-        for (int d = 0; d < PARTS; ++d) S[i][0] = ka_mfma_qk(a, qy[i].op[k][d], S[i][0], 126, Query::scale(d, g));
+      for (int d = 0; d < PARTS; ++d) S[0] = ka_mfma_qk(a, qy.op[k][d], S[0], 126, Query::scale(d, g));
     }
   }
   if (next) ka_load_keys<DT>(next, U, keys);
 
 #pragma unroll
-  for (int i = 0; i < QT; ++i)
+  for (int t = 0; t < 8; ++t)
 #pragma unroll
-    for (int t = 0; t < 8; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) S[i][t][r] *= ks[t][r];
-  // lane group g, scores t, element r: token 64 (t / 4) + 16 g + 4 (t % 4) + r of the page
+    for (int r = 0; r < 4; ++r) S[t][r] *= ks[t][r];
   const int64_t t0 = (int64_t)page * KP_TOKENS;
-  const bool masked = t0 + KP_TOKENS - 1 > rg.min_pos || (p.window && t0 <= rg.max_pos - p.window && t0 + KP_TOKENS > p.sinks);
+  const bool masked = ka_masked(p, rg, t0);
   if (masked) {
-    const int snk = (int)min(max((int64_t)p.sinks - t0, (int64_t)0), (int64_t)KP_TOKENS);
-    auto clamp = [&](int64_t v) { return (int)min(max(v - t0, (int64_t)-1), (int64_t)KP_TOKENS); };
-#pragma unroll
-    for (int i = 0; i < QT; ++i) {
-      // a row sees tokens lo + 1 .. hi of the page, and those below snk
-      const int hi = clamp(qy[i].pos) - 16 * g, lo = (p.window ? clamp(qy[i].pos - p.window) : -1) - 16 * g, sk = snk - 16 * g;
-#pragma unroll
-      for (int t = 0; t < 8; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int j = 64 * (t >> 2) + 4 * (t & 3) + r;
-          S[i][t][r] = j <= hi && (j > lo || j < sk) ? S[i][t][r] : -INFINITY;
-        }
-    }
-    // places that no query of the wave sees may hold anything
-    const int hi = clamp(rg.max_pos) - 16 * g, lo = (p.window ? clamp(rg.min_pos - p.window) : -1) - 16 * g, sk = snk - 16 * g;
+    ka_mask(S, KaSeen(p, t0, qy.pos, qy.pos, 16 * g));
+    KaSeen any(p, t0, rg.min_pos, rg.max_pos, 16 * g);          // places that no query of the wave sees may hold anything
+    asm volatile("" : "+v"(any.hi), "+v"(any.lo), "+v"(any.snk));
 #pragma unroll
     for (int t = 0; t < 8; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int j = 64 * (t >> 2) + 4 * (t & 3) + r;
-        vs[t][r] = j <= hi && (j > lo || j < sk) ? vs[t][r] : 0.0f;
-      }
+      for (int r = 0; r < 4; ++r) vs[t][r] = any.at(ka_token(t, r)) ? vs[t][r] : 0.0f;
   }
 
   // value scales, brought below 2^8 by a power of two 2^(E - 134) that the instruction puts back
   float vm = 0.0f;
+  if (masked) {
 #pragma unroll
-  for (int t = 0; t < 8; ++t) vm = fmaxf(vm, fmaxf(fmaxf(vs[t][0], vs[t][1]), fmaxf(vs[t][2], vs[t][3])));
+    for (int t = 0; t < 8; ++t)
+      vm = ka_max3(ka_max3(vm, ka_finite(vs[t][0]), ka_finite(vs[t][1])), ka_finite(vs[t][2]), ka_finite(vs[t][3]));
+  } else {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) vm = ka_max3(ka_max3(vm, vs[t][0], vs[t][1]), vs[t][2], vs[t][3]);
+  }
   vm = ka_max_groups(vm);
-  const int E = min(max((int)(__float_as_uint(vm) >> 23), 16), 254);
-  const float vf = __uint_as_float((u32)(261 - E) << 23);
+  const int E = ka_exponent(vm);
+  const float vf = ka_scale_factor(E);
 #pragma unroll
   for (int t = 0; t < 8; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) vs[t][r] *= vf;
 
-  v8i ph[QT], pl[QT];
-#pragma unroll
-  for (int i = 0; i < QT; ++i) {
-    float mx = -INFINITY;
-#pragma unroll
-    for (int t = 0; t < 8; ++t) mx = fmaxf(mx, fmaxf(fmaxf(S[i][t][0], S[i][t][1]), fmaxf(S[i][t][2], S[i][t][3])));
-    const float m = fmaxf(st[i].m, ka_max_groups(mx));
-    const float base = m == -INFINITY ? 0.0f : m * qy[i].c;      // nothing seen so far: all terms are exp2(-inf) = 0
-    if (__any(m > st[i].m)) {
-      const float al = __builtin_amdgcn_exp2f(st[i].m * qy[i].c - base);
-      st[i].l *= al;
-#pragma unroll
-      for (int t = 0; t < DT / 16; ++t) st[i].o[t] *= al;
-      st[i].m = m;
-    }
-    if (masked) ka_weights<true>(S[i], vs, qy[i].c, base, st[i].l, ph[i], pl[i]);
-    else ka_weights<false>(S[i], vs, qy[i].c, base, st[i].l, ph[i], pl[i]);
-  }
+  const float base = ka_rescale<DT>(S, qy.c, st);
+  v8i ph, pl;
+  auto scales = [&](int t) { return make_float4(vs[t][0], vs[t][1], vs[t][2], vs[t][3]); };
+  ka_weights(S, scales, qy.c, base, st.l, ph, pl);
 
 #pragma unroll
   for (int d = 0; d < DT / 16; ++d) {
     const auto w = vals.w[d];
     u32 a[4];
     kp_expand(w.a, w.b, w.c, a);
-#pragma unroll
-    for (int i = 0; i < QT; ++i) {
-      st[i].o[d] = ka_mfma_pv(a, ph[i], st[i].o[d], 127, E - 7);
-      st[i].o[d] = ka_mfma_pv(a, pl[i], st[i].o[d], 127, E - 12);
-    }
+    st.o[d] = ka_mfma_pv(a, ph, st.o[d], 127, E - 7);
+    st.o[d] = ka_mfma_pv(a, pl, st.o[d], 127, E - 12);
   }
-  if (page == 0) {
+  if (FIRST) {
 #pragma unroll
     for (int d = 0; d < DT / 16; ++d) {
-      const int ch = min(16 * d, 32 * U - 16) + n;
-      const u32 bit = (lows[U + (ch >> 5)] >> kp_sign_bit(ch & 31)) & 1u;
-      const u32 a[4] = {g == 0 ? bit | (vals.w[d].c & 8u) : 0u, 0u, 0u, 0u};
-#pragma unroll
-      for (int i = 0; i < QT; ++i) {
-        st[i].o[d] = ka_mfma_pv(a, ph[i], st[i].o[d], 126, E - 7);
-        st[i].o[d] = ka_mfma_pv(a, pl[i], st[i].o[d], 126, E - 12);
-      }
+      u32 a[4];
+      ka_low_values(lows, U, d, vals.w[d].c, a);
+      st.o[d] = ka_mfma_pv(a, ph, st.o[d], 126, E - 7);
+      st.o[d] = ka_mfma_pv(a, pl, st.o[d], 126, E - 12);
     }
   }
 }
@@ -443,22 +499,24 @@ __device__ __forceinline__ const unsigned char* ka_next(const KaArgs& p, const K
 }
 
 // All pages of a wave: turns k, k + step, ...
-template <int DT, int QT, bool Q4>
+template <int DT, bool Q4, bool QV>
 __device__ __forceinline__ void ka_walk(const KaArgs& p, const KvSeq& q, const KaRange& rg, int h, int k, int step,
-                                        const KaQuery<DT, Q4> (&qy)[QT], KaState<DT> (&st)[QT]) {
+                                        const KaQuery<DT, Q4, QV>& qy, KaState<DT>& st) {
   const int U = kp_units(p.D), hb = kp_head_bytes(U);
   KaCodes<DT == 256 ? 16 : 8> keys;
   int page = 0;
   const unsigned char* head = ka_next(p, q, rg, h, hb, step, k, page);
   if (head) ka_load_keys<DT>(head, U, keys);
-  while (head) {
+  auto turn = [&](auto first) {
     int page2 = 0;
     k += step;
     const unsigned char* next = ka_next(p, q, rg, h, hb, step, k, page2);
-    ka_page<DT, QT, Q4>(p, rg, page, head, next, U, keys, qy, st);
+    ka_page<decltype(first)::value, DT, Q4, QV>(p, rg, page, head, next, U, keys, qy, st);
     head = next;
     page = page2;
-  }
+  };
+  if (head && page == 0) turn(std::true_type());
+  while (head) turn(std::false_type());
 }
 
 template <int DT>
@@ -482,27 +540,235 @@ __device__ __forceinline__ void ka_store(const KaArgs& p, const KvSeq& q, int r,
   }
 }
 
-// A wave: QT x 16 rows (row = new token x query head of the group) of one key / value head, all their pages.
-template <int DT, int QT, bool Q4>
-__global__ __launch_bounds__(KA_THREADS, DT == 256 ? 1 : 2) void kv_attention_rows_kernel(KaArgs p, int shift, int n_tiles) {
+// Many rows: a workgroup has 4 x QT x 16 rows (row = new token x query head of the group) of one key / value head and walks their
+// pages; each wave widens a quarter of a page's codes into LDS, where all four read them as operands, while the page before is worked
+// on.  That leaves a wave 13 registers for the page to come and a quarter of the widening, and its scales come prepared: a page costs a
+// wave of 32 rows about 650 vector instructions where a wave of its own pages takes 1060, which is what bounds this kernel.
+template <int DT>
+struct KaStage {
+  static constexpr int KT = DT == 64 ? 4 : DT / 16;      // 1 KB pieces of key operands (DT = 64: 16 tokens take half a one)
+  static constexpr int VT = DT / 16;                     // and of value operands
+  uint4 keys[KT * 64], vals[VT * 64];
+  float ks[KP_TOKENS], vs[KP_TOKENS];
+  int E[4];                                              // of tokens 0 .. 63, of tokens 64 .. 127
+};
+template <int DT>
+struct KaRaw {                                           // a wave's share of a page on its way
+  typedef KaCodes<1>::Words Words;
+  Words k[KaStage<DT>::KT / 4], v[KaStage<DT>::VT / 4];
+  float scale;
+};
+
+template <int DT>
+__device__ __forceinline__ void ka_fetch(const unsigned char* head, int U, int wave, KaRaw<DT>& raw) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < KaStage<DT>::KT / 4; ++i) {
+    const int j = 4 * i + wave;                          // piece: 16 tokens x 4 groups of channels (DT = 64: 32 tokens x 2)
+    const int tok = DT == 64 ? 32 * j + 16 * (g >> 1) + n : DT == 128 ? 16 * j + n : 16 * (j >> 1) + n;
+    const int u = min(DT == 64 ? g & 1 : DT == 128 ? g : 4 * (j & 1) + g, U - 1);
+    raw.k[i] = *reinterpret_cast<const typename KaRaw<DT>::Words*>(head + (u32)(tok * U + u) * 12);
+  }
+  const unsigned char* v = head + kp_code_bytes(U);
+#pragma unroll
+  for (int i = 0; i < KaStage<DT>::VT / 4; ++i) {
+    const int ch = min(16 * (4 * i + wave), 32 * U - 16) + n;
+    raw.v[i] = *reinterpret_cast<const typename KaRaw<DT>::Words*>(v + (u32)(ch * 4 + g) * 12);
+  }
+  raw.scale = reinterpret_cast<const float*>(head + kp_scale_off(U))[threadIdx.x];       // waves 0, 1: keys; 2, 3: values
+}
+
+template <int DT>
+__device__ __forceinline__ void ka_widen(const KaArgs& p, const KaRange& rg, int page, int wave, const KaRaw<DT>& raw, KaStage<DT>& to) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < KaStage<DT>::KT / 4; ++i) {
+    u32 a[4];
+    kp_expand(raw.k[i].a, raw.k[i].b, raw.k[i].c, a);
+    to.keys[(4 * i + wave) * 64 + lane] = make_uint4(a[0], a[1], a[2], a[3]);
+  }
+#pragma unroll
+  for (int i = 0; i < KaStage<DT>::VT / 4; ++i) {
+    u32 a[4];
+    kp_expand(raw.v[i].a, raw.v[i].b, raw.v[i].c, a);
+    to.vals[(4 * i + wave) * 64 + lane] = make_uint4(a[0], a[1], a[2], a[3]);
+  }
+  float s = raw.scale;
+  if (wave < 2) {
+    if (page == 0 && threadIdx.x == 0) s *= 2.0f;
+    to.ks[threadIdx.x] = s;
+  } else {
+    const int tok = (int)threadIdx.x - KP_TOKENS;
+    if (page == 0 && tok == 0) s *= 2.0f;
+    // places that no row of the workgroup sees may hold anything
+    if (!KaSeen(p, (int64_t)page * KP_TOKENS, rg.min_pos, rg.max_pos, 0).at(tok)) s = 0.0f;
+    const int E = ka_exponent(__uint_as_float(bl_wave_max_u32(__float_as_uint(ka_finite(s)))));
+    to.vs[tok] = s * ka_scale_factor(E);
+    if (lane == 0) to.E[wave - 2] = E;
+  }
+}
+
+// One page, from LDS, against a wave's QT x 16 queries
+template <bool FIRST, int DT, int QT, bool Q4, bool QV>
+__device__ __forceinline__ void ka_staged(const KaArgs& p, const KaRange& rg, int page, const unsigned char* head, int U,
+                                          const KaStage<DT>& sg, const uint4* digits, const float (&qc)[QT], const int (&qp)[QT],
+                                          KaState<DT> (&st)[QT]) {
+  typedef KaQuery<DT, Q4, QV> Query;
+  constexpr int KS = Query::KS, PARTS = Query::PARTS, WORDS = KS * PARTS * 6;
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int64_t t0 = (int64_t)page * KP_TOKENS;
+  // (The scheduler would fetch all operands at once and spill: fences between steps, the next operand fetched a step ahead.)
+  u32 dg[QT * WORDS];
+#pragma unroll
+  for (int j = 0; j < QT * WORDS / 4; ++j) {
+    const uint4 w = digits[64 * j];
+    dg[4 * j] = w.x; dg[4 * j + 1] = w.y; dg[4 * j + 2] = w.z; dg[4 * j + 3] = w.w;
+  }
+  auto digit = [&](int i, int s, int d) -> const u32 (&)[6] { return *reinterpret_cast<const u32 (*)[6]>(dg + ((i * KS + s) * PARTS + d) * 6); };
+  v4f S[QT][8];
+  auto key = [&](int j) { return DT == 64 ? sg.keys[32 * j + 16 * (g & 1) + n] : sg.keys[j * 64 + lane]; };
+  uint4 ahead = key(0);
+#pragma unroll
+  for (int j = 0; j < 8 * KS; ++j) {
+    const int t = j / KS, s = j % KS;
+    const u32 a[4] = {ahead.x, ahead.y, ahead.z, ahead.w};
+    if (j + 1 < 8 * KS) ahead = key(j + 1);
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      if (s == 0) S[i][t] = (v4f){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int d = 0; d < PARTS; ++d) S[i][t] = ka_mfma_qk(a, digit(i, s, d), S[i][t], 127, Query::scale(d, g));
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  const u32* lows = reinterpret_cast<const u32*>(head + kp_low_off(U));
+  if (FIRST) {                         // the first token's lowest bits (its scales are doubled in LDS)
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int u = min(DT == 64 ? g & 1 : 4 * s + g, U - 1);
+      u32 a[4];
+      ka_low_keys(n == 0 ? lows[u] : 0u, n == 0 ? reinterpret_cast<const u32*>(head)[u * 3 + 2] : 0u, a);
+#pragma unroll
+      for (int i = 0; i < QT; ++i)
+#pragma unroll
+        for (int d = 0; d < PARTS; ++d) S[i][0] = ka_mfma_qk(a, digit(i, s, d), S[i][0], 126, Query::scale(d, g));
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    const float4 s4 = *reinterpret_cast<const float4*>(sg.ks + 16 * g + ka_token(t, 0));
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      S[i][t][0] *= s4.x; S[i][t][1] *= s4.y; S[i][t][2] *= s4.z; S[i][t][3] *= s4.w;
+    }
+  }
+  const bool masked = ka_masked(p, rg, t0);
+  v8i ph[QT], pl[QT];
+  auto scales = [&](int t) { return *reinterpret_cast<const float4*>(sg.vs + 16 * g + ka_token(t, 0)); };
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    if (masked) ka_mask(S[i], KaSeen(p, t0, qp[i], qp[i], 16 * g));
+    const float base = ka_rescale<DT>(S[i], qc[i], st[i]);
+    __builtin_amdgcn_sched_barrier(0);
+    ka_weights(S[i], scales, qc[i], base, st[i].l, ph[i], pl[i]);
+    asm volatile("" : "+v"(ph[i]), "+v"(pl[i]), "+v"(st[i].l));      // (done here, not where it is used)
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  const int E = sg.E[g >> 1];          // (the instruction's scale of 32 tokens is that of their lane group)
+  ahead = sg.vals[lane];
+#pragma unroll
+  for (int d = 0; d < DT / 16; ++d) {
+    const u32 a[4] = {ahead.x, ahead.y, ahead.z, ahead.w};
+    if (d + 1 < DT / 16) ahead = sg.vals[64 * (d + 1) + lane];
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      st[i].o[d] = ka_mfma_pv(a, ph[i], st[i].o[d], 127, E - 7);
+      st[i].o[d] = ka_mfma_pv(a, pl[i], st[i].o[d], 127, E - 12);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (FIRST) {
+#pragma unroll
+    for (int d = 0; d < DT / 16; ++d) {
+      const int ch = min(16 * d, 32 * U - 16) + n;
+      u32 a[4];
+      ka_low_values(lows, U, d, reinterpret_cast<const u32*>(head + kp_code_bytes(U))[ch * 12 + 2], a);
+#pragma unroll
+      for (int i = 0; i < QT; ++i) {
+        st[i].o[d] = ka_mfma_pv(a, ph[i], st[i].o[d], 126, E - 7);
+        st[i].o[d] = ka_mfma_pv(a, pl[i], st[i].o[d], 126, E - 12);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < QT; ++i)
+#pragma unroll
+    for (int d = 0; d < DT / 16; ++d) asm volatile("" : "+v"(st[i].o[d]));
+}
+
+template <int DT, int QT, bool Q4, bool QV>
+__global__ __launch_bounds__(KA_THREADS, 2) void kv_attention_rows_kernel(KaArgs p, int shift, int n_tiles) {
+  extern __shared__ __align__(16) unsigned char ka_smem[];
+  KaStage<DT>* stage = reinterpret_cast<KaStage<DT>*>(ka_smem);
+  typedef KaQuery<DT, Q4, QV> Query;
   const int h = (int)(blockIdx.x % (unsigned)p.H);
   // late rows have the most pages: they go first
   const int64_t item = n_tiles - 1 - (int64_t)(blockIdx.x / (unsigned)p.H);
   KvSeq q;
   const int64_t local = kp_find(p.b, item, p.G, shift, 1, q);
-  if (local < 0) return;
+  if (local < 0) return;                   // (whole workgroup)
   const int rows = q.n * p.G;              // (at most T * G, which the host bounds)
-  const int64_t first = (local << shift) + (int64_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (16 * QT);
-  if (first >= rows) return;               // (no barriers in this kernel)
-  const int r0 = (int)first, n = threadIdx.x & 15;
-  KaQuery<DT, Q4> qy[QT];
+  if ((local << shift) >= rows) return;
+  const int block0 = (int)(local << shift), n = threadIdx.x & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r0 = block0 + wave * (16 * QT);
+  const bool live = r0 < rows;             // (a wave without rows still widens its share)
+  // a wave's digits stay in LDS (36 words a lane that the registers have no room for), each lane's written and read by itself
+  constexpr int WORDS = QT * Query::KS * Query::PARTS * 6;
+  uint4* digits = reinterpret_cast<uint4*>(ka_smem + 2 * sizeof(KaStage<DT>)) + wave * (WORDS / 4 * 64) + (threadIdx.x & 63);
+  float qc[QT];
+  int qp[QT];
   KaState<DT> st[QT];
+  {
+    u32 w[WORDS];
 #pragma unroll
-  for (int i = 0; i < QT; ++i) {
-    qy[i].load(p, q, r0 + 16 * i + n, rows, h);
-    st[i].clear();
+    for (int i = 0; i < QT; ++i) {
+      Query qy;
+      qy.load(p, q, r0 + 16 * i + n, rows, h);
+      qc[i] = qy.c;
+      qp[i] = qy.pos;
+#pragma unroll
+      for (int e = 0; e < WORDS / QT; ++e) w[i * (WORDS / QT) + e] = (&qy.op[0][0][0])[e];
+      st[i].clear();
+    }
+#pragma unroll
+    for (int j = 0; j < WORDS / 4; ++j) digits[64 * j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
   }
-  ka_walk<DT, QT, Q4>(p, q, ka_range(p, q, r0, 16 * QT, rows), h, 0, 1, qy, st);
+  const KaRange all = ka_range(p, q, block0, KA_WAVES * 16 * QT, rows), rg = ka_range(p, q, live ? r0 : block0, 16 * QT, rows);
+  const int U = kp_units(p.D), hb = kp_head_bytes(U);
+  KaRaw<DT> raw;
+  int k = 0, page = 0, cur = 0;
+  const unsigned char* head = ka_next(p, q, all, h, hb, 1, k, page);
+  if (head) {
+    ka_fetch<DT>(head, U, wave, raw);
+    ka_widen<DT>(p, all, page, wave, raw, stage[0]);
+  }
+  __syncthreads();
+  auto turn = [&](auto first) {
+    int page2 = 0;
+    ++k;
+    const unsigned char* next = ka_next(p, q, all, h, hb, 1, k, page2);
+    if (next) ka_fetch<DT>(next, U, wave, raw);
+    ka_staged<decltype(first)::value, DT, QT, Q4, QV>(p, rg, page, head, U, stage[cur], digits, qc, qp, st);
+    // the other buffer was last read a page ago, before the barrier that ended it
+    if (next) ka_widen<DT>(p, all, page2, wave, raw, stage[cur ^ 1]);
+    __syncthreads();
+    head = next;
+    page = page2;
+    cur ^= 1;
+  };
+  if (head && page == 0) turn(std::true_type());
+  while (head) turn(std::false_type());
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
     float l = st[i].l;
@@ -517,7 +783,7 @@ __global__ __launch_bounds__(KA_THREADS, DT == 256 ? 1 : 2) void kv_attention_ro
 // Partial results of (tile, head, split): 16 rows x (log2 maximum, sum), then 16 x DT outputs.
 __host__ __device__ static inline int64_t ka_part_floats(int DT) { return 16 * (DT + 2); }
 
-template <int DT, bool Q4>
+template <int DT, bool Q4, bool QV>
 __global__ __launch_bounds__(KA_THREADS, DT == 256 ? 1 : 2) void kv_attention_split_kernel(KaArgs p) {
   __shared__ float lds_o[KA_WAVES - 1][16][DT + 4];
   __shared__ float lds_m[KA_WAVES][16], lds_l[KA_WAVES][16];
@@ -532,11 +798,11 @@ __global__ __launch_bounds__(KA_THREADS, DT == 256 ? 1 : 2) void kv_attention_sp
   if ((local << 4) >= rows) return;
   const int r0 = (int)(local << 4), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  KaQuery<DT, Q4> qy[1];
+  KaQuery<DT, Q4, QV> qy[1];
   KaState<DT> st[1];
   qy[0].load(p, q, r0 + n, rows, h);
   st[0].clear();
-  ka_walk<DT, 1, Q4>(p, q, ka_range(p, q, r0, 16, rows), h, split * KA_WAVES + wave, p.splits * KA_WAVES, qy, st);
+  ka_walk<DT, Q4, QV>(p, q, ka_range(p, q, r0, 16, rows), h, split * KA_WAVES + wave, p.splits * KA_WAVES, qy[0], st[0]);
   float l = st[0].l;
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
@@ -576,6 +842,7 @@ __global__ __launch_bounds__(KA_THREADS, DT == 256 ? 1 : 2) void kv_attention_sp
     return;
   }
   float* part = p.part + ((item * p.H + h) * p.splits + split) * ka_part_floats(DT);
+  if (r0 + n >= rows) return;
   if (g == 0) {
     part[n] = top;
     part[16 + n] = sum;
@@ -660,7 +927,6 @@ int bl_launch_kv_attention(const void* Q, int64_t ldq, bl_dtype qdt, int Hq, int
   KaArgs p;
   p.Q = Q; p.ldq = ldq; p.n_pos = n_pos;
   p.q_f32 = qdt == BL_F32;
-  p.q_vec = D % 32 == 0 && bl_aligned16(Q) && ldq * (qdt == BL_F32 ? 4 : 2) % 16 == 0;
   p.Hq = Hq; p.H = H; p.G = Hq / H; p.D = D;
   p.b = b; p.rope = rope;
   p.cs = scale * 1.44269504f;
@@ -670,32 +936,39 @@ int bl_launch_kv_attention(const void* Q, int64_t ldq, bl_dtype qdt, int Hq, int
   p.O = (uint16_t*)O; p.part = (float*)ws;
   p.splits = ka_splits(b.T, b.n_seqs, p.G, H, b.max_pages);
   const int dt = ka_dt(D);
-  if (p.splits) {
-    const int64_t tiles = ka_tiles(b.T, p.G, b.n_seqs, 4) * H;
-    if (!bl_grid_ok(tiles * p.splits) || !bl_grid_ok(tiles * 16)) return BL_ESHAPE;
-    const unsigned blocks = (unsigned)(tiles * p.splits);
-#define KA_GO(DT)                                                                    \
-  do {                                                                               \
-    if (q_bits == 4) kv_attention_split_kernel<DT, true><<<blocks, KA_THREADS, 0, s>>>(p); \
-    else kv_attention_split_kernel<DT, false><<<blocks, KA_THREADS, 0, s>>>(p);      \
-    BL_HIP_CHECK_LAUNCH();                                                           \
-    if (p.splits > 1) kv_attention_join_kernel<DT><<<(unsigned)(tiles * 16), KA_THREADS, 0, s>>>(p); \
+  const bool qv = qdt == BL_BF16 && D % 32 == 0 && bl_aligned16(Q) && ldq % 8 == 0 && bl_aligned16(rope);
+#define KA_GO2(DT, Q4, QV)                                                                               \
+  do {                                                                                                   \
+    if (p.splits) kv_attention_split_kernel<DT, Q4, QV><<<blocks, KA_THREADS, 0, s>>>(p);                \
+    else {                                                                                               \
+      constexpr int lds = (int)(2 * sizeof(KaStage<DT>)) + KA_WAVES * 64 * 4 * KA_QT(DT) * KaQuery<DT, Q4, QV>::WORDS; \
+      BL_SET_MAX_LDS_ONCE((kv_attention_rows_kernel<DT, KA_QT(DT), Q4, QV>), lds);                       \
+      kv_attention_rows_kernel<DT, KA_QT(DT), Q4, QV><<<blocks, KA_THREADS, lds, s>>>(p, shift, (int)tiles); \
+    }                                                                                                    \
   } while (0)
-    if (dt == 64) KA_GO(64); else if (dt == 128) KA_GO(128); else KA_GO(256);
-#undef KA_GO
-  } else {
-    const int shift = 6;                   // four waves of 16 rows
-    const int64_t tiles = ka_tiles(b.T, p.G, b.n_seqs, shift);
-    if (!bl_grid_ok(tiles * H)) return BL_ESHAPE;
-    const unsigned blocks = (unsigned)(tiles * H);
-#define KA_GO(DT)                                                                    \
-  do {                                                                               \
-    if (q_bits == 4) kv_attention_rows_kernel<DT, 1, true><<<blocks, KA_THREADS, 0, s>>>(p, shift, (int)tiles); \
-    else kv_attention_rows_kernel<DT, 1, false><<<blocks, KA_THREADS, 0, s>>>(p, shift, (int)tiles); \
+#define KA_GO(DT)                                                  \
+  do {                                                             \
+    if (q_bits == 4) {                                             \
+      if (qv) KA_GO2(DT, true, true); else KA_GO2(DT, true, false); \
+    } else {                                                       \
+      if (qv) KA_GO2(DT, false, true); else KA_GO2(DT, false, false); \
+    }                                                              \
   } while (0)
-    if (dt == 64) KA_GO(64); else if (dt == 128) KA_GO(128); else KA_GO(256);
-#undef KA_GO
-  }
+  const int shift = p.splits ? 4 : 6 + (KA_QT(dt) == 2);           // four waves of KA_QT tiles of 16 rows
+  const int64_t tiles = ka_tiles(b.T, p.G, b.n_seqs, shift);
+  const int64_t n_blocks = tiles * H * (p.splits ? p.splits : 1);
+  if (!bl_grid_ok(n_blocks) || !bl_grid_ok(tiles * H * 16)) return BL_ESHAPE;
+  const unsigned blocks = (unsigned)n_blocks;
+  if (dt == 64) KA_GO(64); else if (dt == 128) KA_GO(128); else KA_GO(256);
   BL_HIP_CHECK_LAUNCH();
+  if (p.splits > 1) {
+    const unsigned joins = (unsigned)(tiles * H * 16);
+    if (dt == 64) kv_attention_join_kernel<64><<<joins, KA_THREADS, 0, s>>>(p);
+    else if (dt == 128) kv_attention_join_kernel<128><<<joins, KA_THREADS, 0, s>>>(p);
+    else kv_attention_join_kernel<256><<<joins, KA_THREADS, 0, s>>>(p);
+    BL_HIP_CHECK_LAUNCH();
+  }
+#undef KA_GO
+#undef KA_GO2
   return BL_OK;
 }
