@@ -4,7 +4,7 @@
 // in one pass over the keys, with the running maximum and sum of the softmax in float32.
 //
 // Both products run on the block-float instruction 16 x 16 x 128, which contracts over a page's 128 tokens.  The cache's codes are
-// sign and two magnitude bits: the nibble of the E2M1 value code / 2, so 32 codes widen to an operand with 13 shifts and masks and
+// sign and two magnitude bits: the nibble of the E2M1 value code / 2, so 32 codes widen to an operand with 11 shifts and masks and
 // are exact.
 //   Queries are fixed-point numbers of the row's largest channel: three digits -15 .. 15, -8 .. 8, -8 .. 8 in E2M3 (whose codes 0 ..
 // 15 are the values 0 .. 15 eighths), a sixteenth apart through the instruction's scale operand; what is lost is at most 1 / 7680
@@ -48,10 +48,9 @@ __device__ __forceinline__ v4f ka_mfma_pv(const u32 (&a)[4], v8i b, v4f c, int s
   const v8i av = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, b, c, 4 /* rows: E2M1 */, 0 /* columns: E4M3 */, 0, sa, 0, sb);
 }
-__device__ __forceinline__ v4f ka_mfma_qk(const u32 (&a)[4], const u32 (&b)[6], v4f c, int sa, int sb) {
+__device__ __forceinline__ v4f ka_mfma_qk(const u32 (&a)[4], v8i b, v4f c, int sa, int sb) {      // (six words of b)
   const v8i av = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
-  const v8i bv = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], (int)b[4], (int)b[5], 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, c, 4 /* rows: E2M1 */, 2 /* columns: E2M3 */, 0, sa, 0, sb);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, b, c, 4 /* rows: E2M1 */, 2 /* columns: E2M3 */, 0, sa, 0, sb);
 }
 
 // Four floats below 2^8 as hi + 2^-5 lo, both E4M3.  `old`: any value (the conversions write a half each).
@@ -69,7 +68,16 @@ __device__ __forceinline__ float ka_max3(float a, float b, float c) {
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
   return r;
 }
-__device__ __forceinline__ float ka_max_groups(float v) {      // over the four lanes of a query
+// v of the lane 4 or 8 further in its row of 16, wrapping round
+template <int O>
+__device__ __forceinline__ float ka_ror(float v) {
+  return __uint_as_float((u32)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + O, 0xF, 0xF, false));
+}
+// over the lanes of a query: R = 16 the four of a column, R < 16 also those R columns apart
+template <int R = 16>
+__device__ __forceinline__ float ka_max_groups(float v) {
+  if (R <= 8) v = fmaxf(v, ka_ror<8>(v));
+  if (R <= 4) v = fmaxf(v, ka_ror<4>(v));
   v = fmaxf(v, __shfl_xor(v, 16, 64));
   return fmaxf(v, __shfl_xor(v, 32, 64));
 }
@@ -99,7 +107,7 @@ struct KaQuery {
   static constexpr int KS = DT == 256 ? 2 : 1;
   static constexpr int PARTS = Q4 ? 1 : DT == 64 ? 2 : 3;
   static constexpr int WORDS = KS * PARTS * 6;
-  u32 op[KS][PARTS][6];
+  v8i op[KS][PARTS];                       // six words each
   float c;                                 // log2 units of a score that is product * key scale
   int pos;                                 // position; -1: no such row
 
@@ -194,10 +202,7 @@ struct KaQuery {
     c = fmaxf(16.0f * p.cs * (top / lv), 1.17549435e-38f);      // digits are eighths, codes halves; never 0 (times -inf)
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
-#pragma unroll
-      for (int w = 0; w < PARTS; ++w)
-#pragma unroll
-        for (int e = 0; e < 6; ++e) op[k][w][e] = 0;
+      u32 code[PARTS][32];
 #pragma unroll
       for (int e = 0; e < 32; ++e) {
         // magnitude in 256ths of a unit: the digits are its three nibbles, the sign is theirs alike
@@ -209,12 +214,19 @@ struct KaQuery {
           if (g >= 2) { d[0] = Q4 ? 0u : d[1]; d[1] = 0u; } else d[1] = d[2];
         }
 #pragma unroll
-        for (int w = 0; w < PARTS; ++w) {
-          const u32 code = d[w] | sg;
-          const int bit = 6 * e;
-          op[k][w][bit >> 5] |= code << (bit & 31);
-          if ((bit & 31) > 26) op[k][w][(bit >> 5) + 1] |= code >> (32 - (bit & 31));
+        for (int w = 0; w < PARTS; ++w) code[w][e] = d[w] | sg;
+      }
+#pragma unroll
+      for (int w = 0; w < PARTS; ++w) {
+        u32 o[6];
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {      // 16 codes of 6 bits in three words
+          const u32* c6 = code[w] + 16 * v;
+          o[3 * v] = c6[0] | c6[1] << 6 | c6[2] << 12 | c6[3] << 18 | c6[4] << 24 | c6[5] << 30;
+          o[3 * v + 1] = c6[5] >> 2 | c6[6] << 4 | c6[7] << 10 | c6[8] << 16 | c6[9] << 22 | c6[10] << 28;
+          o[3 * v + 2] = c6[10] >> 4 | c6[11] << 2 | c6[12] << 8 | c6[13] << 14 | c6[14] << 20 | c6[15] << 26;
         }
+        op[k][w] = (v8i){(int)o[0], (int)o[1], (int)o[2], (int)o[3], (int)o[4], (int)o[5], 0, 0};
       }
     }
   }
@@ -255,15 +267,11 @@ __device__ __forceinline__ KaRange ka_range(const KaArgs& p, const KvSeq& q, int
   return w;
 }
 
-// A page's codes as they come: 12 bytes for 32 codes.  Loads are issued together and used later.
-template <int N>
-struct KaCodes {
-  struct __align__(4) Words { u32 a, b, c; };
-  Words w[N];
-};
+// A page's codes as they come: 12 bytes for 32 codes.
+struct __align__(4) KaWords { u32 a, b, c; };
 
 template <int DT>
-__device__ __forceinline__ void ka_load_keys(const unsigned char* head, int U, KaCodes<DT == 256 ? 16 : 8>& r) {
+__device__ __forceinline__ void ka_load_keys(const unsigned char* head, int U, KaWords (&r)[DT == 256 ? 16 : 8]) {
   constexpr int KS = DT == 256 ? 2 : 1;
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
 #pragma unroll
@@ -272,27 +280,15 @@ __device__ __forceinline__ void ka_load_keys(const unsigned char* head, int U, K
     const int u = min(DT == 64 ? g & 1 : 4 * k + g, U - 1);
     const u32 off = (u32)(n * U + u) * 12;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) r.w[t * KS + k] = *reinterpret_cast<const typename KaCodes<DT == 256 ? 16 : 8>::Words*>(head + off + t * 16 * 12 * U);
+    for (int t = 0; t < 8; ++t) r[t * KS + k] = *reinterpret_cast<const KaWords*>(head + off + t * 16 * 12 * U);
   }
 }
+// codes of 16 of the values' channels
 template <int DT>
-__device__ __forceinline__ void ka_load_values(const unsigned char* head, int U, KaCodes<DT / 16>& r) {
+__device__ __forceinline__ KaWords ka_load_values(const unsigned char* head, int U, int d) {
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-  const unsigned char* v = head + kp_code_bytes(U);
-#pragma unroll
-  for (int d = 0; d < DT / 16; ++d) {
-    const int ch = min(16 * d, 32 * U - 16) + n;    // (channels that the head lacks are not stored)
-    r.w[d] = *reinterpret_cast<const typename KaCodes<DT / 16>::Words*>(v + (u32)(ch * 4 + g) * 12);
-  }
-}
-// 128 scales: t of a lane are those of tokens 64 (t / 4) + 16 g + 4 (t % 4) ...
-__device__ __forceinline__ void ka_load_scales(const float* s, float (&v)[8][4]) {
-  const int g = (threadIdx.x & 63) >> 4;
-#pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    const float4 w = *reinterpret_cast<const float4*>(s + 64 * (t >> 2) + 16 * g + 4 * (t & 3));
-    v[t][0] = w.x; v[t][1] = w.y; v[t][2] = w.z; v[t][3] = w.w;
-  }
+  const int ch = min(16 * d, 32 * U - 16) + n;      // (channels that the head lacks are not stored)
+  return *reinterpret_cast<const KaWords*>(head + kp_code_bytes(U) + (u32)(ch * 4 + g) * 12);
 }
 
 // a * b, and 0 where either is 0, whatever the other is (the instruction, so that the compiler knows of it)
@@ -300,11 +296,11 @@ extern "C" __device__ float ka_mul_legacy(float a, float b) __asm("llvm.amdgcn.f
 
 // Probabilities of 16 queries as the second product's operands; scales(t): the four value scales of scores t.  What is not seen has
 // probability 0, and 0 times a scale that is infinite or no number is 0 here.
-template <typename F>
-__device__ __forceinline__ void ka_weights(const v4f (&S)[8], F scales, float c, float base, float& l, v8i& ph, v8i& pl) {
+template <int N, typename F>
+__device__ __forceinline__ void ka_weights(const v4f (&S)[N], F scales, float c, float base, float& l, int (&ph)[N], int (&pl)[N]) {
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int t = 0; t < 8; ++t) {
+  for (int t = 0; t < N; ++t) {
     const float4 s4 = scales(t);
     const float vs[4] = {s4.x, s4.y, s4.z, s4.w};
     float w[4];
@@ -314,10 +310,7 @@ __device__ __forceinline__ void ka_weights(const v4f (&S)[8], F scales, float c,
       sum[r] += e;
       w[r] = ka_mul_legacy(e, vs[r]);
     }
-    int hi, lo;
-    ka_split4(w, __float_as_int(S[t][0]), hi, lo);
-    ph[t] = hi;
-    pl[t] = lo;
+    ka_split4(w, __float_as_int(S[t][0]), ph[t], pl[t]);
   }
   l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
@@ -355,25 +348,27 @@ struct KaSeen {
   }
   __device__ __forceinline__ bool at(int j) const { return j <= hi && (j > lo || j < snk); }
 };
-// lane group g, scores t, element r: token 64 (t / 4) + 16 g + 4 (t % 4) + r of the page
+// Scores t, element r of lane group g are those of token 64 (t / 4) + 4 (t % 4) + r + 16 g of the page
 __device__ __forceinline__ constexpr int ka_token(int t, int r) { return 64 * (t >> 2) + 4 * (t & 3) + r; }
 
-__device__ __forceinline__ void ka_mask(v4f (&S)[8], KaSeen see) {
+// N scores of four, every STEP-th t; `see` less what the lane adds to ka_token
+template <int STEP, int N>
+__device__ __forceinline__ void ka_mask(v4f (&S)[N], KaSeen see) {
   // (without a window most comparisons are the same for every page: kept here, not held in registers over the loop)
   asm volatile("" : "+v"(see.hi), "+v"(see.lo), "+v"(see.snk));
 #pragma unroll
-  for (int t = 0; t < 8; ++t)
+  for (int t = 0; t < N; ++t)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) S[t][r] = see.at(ka_token(t, r)) ? S[t][r] : -INFINITY;
+    for (int r = 0; r < 4; ++r) S[t][r] = see.at(ka_token(STEP * t, r)) ? S[t][r] : -INFINITY;
 }
 
 // New maximum over a page's scores, what was summed so far brought to it; -> the maximum in log2 units
-template <int DT>
-__device__ __forceinline__ float ka_rescale(const v4f (&S)[8], float c, KaState<DT>& st) {
+template <int DT, int R, int N>
+__device__ __forceinline__ float ka_rescale(const v4f (&S)[N], float c, KaState<DT>& st) {
   float mx = -INFINITY;
 #pragma unroll
-  for (int t = 0; t < 8; ++t) mx = ka_max3(ka_max3(mx, S[t][0], S[t][1]), S[t][2], S[t][3]);
-  const float m = fmaxf(st.m, ka_max_groups(mx));
+  for (int t = 0; t < N; ++t) mx = ka_max3(ka_max3(mx, S[t][0], S[t][1]), S[t][2], S[t][3]);
+  const float m = fmaxf(st.m, ka_max_groups<R>(mx));
   const float base = m == -INFINITY ? 0.0f : m * c;      // nothing seen so far: all terms are exp2(-inf) = 0
   if (__any(m > st.m)) {
     const float al = __builtin_amdgcn_exp2f(st.m * c - base);
@@ -385,105 +380,128 @@ __device__ __forceinline__ float ka_rescale(const v4f (&S)[8], float c, KaState<
   return base;
 }
 
-// One page against 16 queries.  keys: the page's key codes; on return those of `next` (nullptr: none) are on their way.  Values and
-// scales are fetched with the scores' products ahead of them.
-// FIRST: the sequence's page 0.
-template <bool FIRST, int DT, bool Q4, bool QV>
+// A lane's scales: those of its scores' tokens
+template <int STEP, int N>
+__device__ __forceinline__ void ka_load_scales(const float* s, int base, float (&v)[N][4]) {
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    const float4 w = *reinterpret_cast<const float4*>(s + base + ka_token(STEP * t, 0));
+    v[t][0] = w.x; v[t][1] = w.y; v[t][2] = w.z; v[t][3] = w.w;
+  }
+}
+
+// What a wave has of the page it works on.  Each part is replaced by the next page's as soon as it has been used, so that a page's
+// loads are on their way for the time a whole page takes.
+template <int DT, int N>
+struct KaHeld {
+  KaWords keys[DT == 256 ? 16 : 8], vals[DT / 16];
+  float ks[N][4], vs[N][4];
+};
+
+// One page against R queries.  w: the page's; on return what `next` (a page that can be read) has.  FIRST: the sequence's page 0.
+// R < 16: the products have 16 columns whatever is in them, so every query stands in 16 / R of them, and of these column j works on
+// the scores t = j, j + 16 / R, ... alone: the softmax takes R / 16 of the instructions.  As the second product's operand a column has
+// zeros for the others' tokens; the columns' outputs are added up after the last page.
+template <bool FIRST, int DT, int R, bool Q4, bool QV>
 __device__ __forceinline__ void ka_page(const KaArgs& p, const KaRange& rg, int page, const unsigned char* head,
-                                        const unsigned char* next, int U, KaCodes<DT == 256 ? 16 : 8>& keys,
-                                        const KaQuery<DT, Q4, QV>& qy, KaState<DT>& st) {
+                                        const unsigned char* next, int U, KaHeld<DT, R / 2>& w, const KaQuery<DT, Q4, QV>& qy,
+                                        KaState<DT>& st) {
   typedef KaQuery<DT, Q4, QV> Query;
-  constexpr int KS = Query::KS, PARTS = Query::PARTS;
-  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-  const float* k_scale = reinterpret_cast<const float*>(head + kp_scale_off(U));
+  constexpr int KS = Query::KS, PARTS = Query::PARTS, STEP = 16 / R, N = 8 / STEP;
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, j = n / R;
+  const int base_tok = 16 * g + 4 * j;
   const u32* lows = reinterpret_cast<const u32*>(head + kp_low_off(U));
-  float ks[8][4], vs[8][4];
-  KaCodes<DT / 16> vals;
-  ka_load_scales(k_scale, ks);
-  ka_load_values<DT>(head, U, vals);
-  ka_load_scales(k_scale + KP_TOKENS, vs);
+  const float* next_scale = reinterpret_cast<const float*>(next + kp_scale_off(U));
 
-  v4f S[8];
+  v4f S[N];
 #pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    S[t] = (v4f){0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < N; ++i) {
+    v4f T[STEP];
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      u32 a[4];
-      const auto w = keys.w[t * KS + k];
-      kp_expand(w.a, w.b, w.c, a);
+    for (int e = 0; e < STEP; ++e) {
+      const int t = STEP * i + e;
+      T[e] = (v4f){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int d = 0; d < PARTS; ++d) S[t] = ka_mfma_qk(a, qy.op[k][d], S[t], 127, Query::scale(d, g));
+      for (int k = 0; k < KS; ++k) {
+        u32 a[4];
+        const KaWords c = w.keys[t * KS + k];
+        kp_expand(c.a, c.b, c.c, a);
+#pragma unroll
+        for (int d = 0; d < PARTS; ++d) T[e] = ka_mfma_qk(a, qy.op[k][d], T[e], 127, Query::scale(d, g));
+        if (FIRST && t == 0) {             // the first token's lowest bits
+          const u32 L = n == 0 ? lows[min(DT == 64 ? g & 1 : 4 * k + g, U - 1)] : 0u;
+          ka_low_keys(L, c.c, a);
+#pragma unroll
+          for (int d = 0; d < PARTS; ++d) T[0] = ka_mfma_qk(a, qy.op[k][d], T[0], 126, Query::scale(d, g));
+        }
+      }
     }
-  }
-  if (FIRST) {                             // the first token's lowest bits
-    if (g == 0) { ks[0][0] *= 2.0f; vs[0][0] *= 2.0f; }
+    S[i] = T[0];
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      const u32 L = n == 0 ? lows[min(DT == 64 ? g & 1 : 4 * k + g, U - 1)] : 0u;
-      u32 a[4];
-      ka_low_keys(L, keys.w[k].c, a);
+    for (int e = 1; e < STEP; ++e)
 #pragma unroll
-      for (int d = 0; d < PARTS; ++d) S[0] = ka_mfma_qk(a, qy.op[k][d], S[0], 126, Query::scale(d, g));
-    }
+      for (int r = 0; r < 4; ++r) S[i][r] = j == e ? T[e][r] : S[i][r];
   }
-  if (next) ka_load_keys<DT>(next, U, keys);
+  ka_load_keys<DT>(next, U, w.keys);
+  if (FIRST && base_tok == 0) { w.ks[0][0] *= 2.0f; w.vs[0][0] *= 2.0f; }
 
 #pragma unroll
-  for (int t = 0; t < 8; ++t)
+  for (int t = 0; t < N; ++t)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) S[t][r] *= ks[t][r];
+    for (int r = 0; r < 4; ++r) S[t][r] *= w.ks[t][r];
+  ka_load_scales<STEP>(next_scale, base_tok, w.ks);
   const int64_t t0 = (int64_t)page * KP_TOKENS;
-  const bool masked = ka_masked(p, rg, t0);
-  if (masked) {
-    ka_mask(S, KaSeen(p, t0, qy.pos, qy.pos, 16 * g));
-    KaSeen any(p, t0, rg.min_pos, rg.max_pos, 16 * g);          // places that no query of the wave sees may hold anything
+  float vm = 0.0f;
+  if (ka_masked(p, rg, t0)) {
+    ka_mask<STEP>(S, KaSeen(p, t0, qy.pos, qy.pos, base_tok));
+    KaSeen any(p, t0, rg.min_pos, rg.max_pos, base_tok);        // places that no query of the wave sees may hold anything
     asm volatile("" : "+v"(any.hi), "+v"(any.lo), "+v"(any.snk));
 #pragma unroll
-    for (int t = 0; t < 8; ++t)
+    for (int t = 0; t < N; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) vs[t][r] = any.at(ka_token(t, r)) ? vs[t][r] : 0.0f;
+      for (int r = 0; r < 4; ++r) {
+        w.vs[t][r] = any.at(ka_token(STEP * t, r)) ? w.vs[t][r] : 0.0f;
+        vm = fmaxf(vm, ka_finite(w.vs[t][r]));
+      }
+  } else {
+#pragma unroll
+    for (int t = 0; t < N; ++t) vm = ka_max3(ka_max3(vm, w.vs[t][0], w.vs[t][1]), w.vs[t][2], w.vs[t][3]);
   }
 
   // value scales, brought below 2^8 by a power of two 2^(E - 134) that the instruction puts back
-  float vm = 0.0f;
-  if (masked) {
-#pragma unroll
-    for (int t = 0; t < 8; ++t)
-      vm = ka_max3(ka_max3(vm, ka_finite(vs[t][0]), ka_finite(vs[t][1])), ka_finite(vs[t][2]), ka_finite(vs[t][3]));
-  } else {
-#pragma unroll
-    for (int t = 0; t < 8; ++t) vm = ka_max3(ka_max3(vm, vs[t][0], vs[t][1]), vs[t][2], vs[t][3]);
-  }
-  vm = ka_max_groups(vm);
+  vm = ka_max_groups<R>(vm);
   const int E = ka_exponent(vm);
   const float vf = ka_scale_factor(E);
 #pragma unroll
-  for (int t = 0; t < 8; ++t)
+  for (int t = 0; t < N; ++t)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) vs[t][r] *= vf;
+    for (int r = 0; r < 4; ++r) w.vs[t][r] *= vf;
 
-  const float base = ka_rescale<DT>(S, qy.c, st);
+  const float base = ka_rescale<DT, R>(S, qy.c, st);
+  int wh[N], wl[N];
+  auto scales = [&](int t) { return make_float4(w.vs[t][0], w.vs[t][1], w.vs[t][2], w.vs[t][3]); };
+  ka_weights(S, scales, qy.c, base, st.l, wh, wl);
+  ka_load_scales<STEP>(next_scale + KP_TOKENS, base_tok, w.vs);
   v8i ph, pl;
-  auto scales = [&](int t) { return make_float4(vs[t][0], vs[t][1], vs[t][2], vs[t][3]); };
-  ka_weights(S, scales, qy.c, base, st.l, ph, pl);
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    ph[t] = STEP == 1 || j == t % STEP ? wh[t / STEP] : 0;
+    pl[t] = STEP == 1 || j == t % STEP ? wl[t / STEP] : 0;
+  }
 
 #pragma unroll
   for (int d = 0; d < DT / 16; ++d) {
-    const auto w = vals.w[d];
+    const KaWords c = w.vals[d];
     u32 a[4];
-    kp_expand(w.a, w.b, w.c, a);
+    kp_expand(c.a, c.b, c.c, a);
     st.o[d] = ka_mfma_pv(a, ph, st.o[d], 127, E - 7);
     st.o[d] = ka_mfma_pv(a, pl, st.o[d], 127, E - 12);
-  }
-  if (FIRST) {
-#pragma unroll
-    for (int d = 0; d < DT / 16; ++d) {
-      u32 a[4];
-      ka_low_values(lows, U, d, vals.w[d].c, a);
+    if (FIRST) {
+      ka_low_values(lows, U, d, c.c, a);
       st.o[d] = ka_mfma_pv(a, ph, st.o[d], 126, E - 7);
       st.o[d] = ka_mfma_pv(a, pl, st.o[d], 126, E - 12);
     }
+    w.vals[d] = ka_load_values<DT>(next, U, d);
   }
 }
 
@@ -492,30 +510,38 @@ __device__ __forceinline__ const unsigned char* ka_next(const KaArgs& p, const K
                                                         int& k, int& page) {
   for (; k < rg.n; k += step) {
     page = k < rg.n_sink ? k : rg.lo + k - rg.n_sink;
-    const int id = p.b.table[(int64_t)q.s * p.b.max_pages + page];
+    const int id = kp_scalar(p.b.table, (int64_t)q.s * p.b.max_pages + page);
     if (id >= 0 && id < p.b.n_pages) return p.pages + ((int64_t)id * p.H + h) * head_bytes;
   }
   return nullptr;
 }
 
 // All pages of a wave: turns k, k + step, ...
-template <int DT, bool Q4, bool QV>
+template <int DT, int R, bool Q4, bool QV>
 __device__ __forceinline__ void ka_walk(const KaArgs& p, const KvSeq& q, const KaRange& rg, int h, int k, int step,
                                         const KaQuery<DT, Q4, QV>& qy, KaState<DT>& st) {
+  constexpr int STEP = 16 / R;
   const int U = kp_units(p.D), hb = kp_head_bytes(U);
-  KaCodes<DT == 256 ? 16 : 8> keys;
+  KaHeld<DT, R / 2> w;
   int page = 0;
   const unsigned char* head = ka_next(p, q, rg, h, hb, step, k, page);
-  if (head) ka_load_keys<DT>(head, U, keys);
-  auto turn = [&](auto first) {
+  if (!head) return;
+  const int lane = threadIdx.x & 63, base_tok = 16 * (lane >> 4) + 4 * ((lane & 15) / R);
+  const float* scales = reinterpret_cast<const float*>(head + kp_scale_off(U));
+  ka_load_keys<DT>(head, U, w.keys);
+  ka_load_scales<STEP>(scales, base_tok, w.ks);
+  ka_load_scales<STEP>(scales + KP_TOKENS, base_tok, w.vs);
+#pragma unroll
+  for (int d = 0; d < DT / 16; ++d) w.vals[d] = ka_load_values<DT>(head, U, d);
+  auto turn = [&](auto first) __attribute__((always_inline)) {
     int page2 = 0;
     k += step;
     const unsigned char* next = ka_next(p, q, rg, h, hb, step, k, page2);
-    ka_page<decltype(first)::value, DT, Q4, QV>(p, rg, page, head, next, U, keys, qy, st);
+    ka_page<decltype(first)::value, DT, R, Q4, QV>(p, rg, page, head, next ? next : head, U, w, qy, st);
     head = next;
     page = page2;
   };
-  if (head && page == 0) turn(std::true_type());
+  if (page == 0) turn(std::true_type());
   while (head) turn(std::false_type());
 }
 
@@ -554,8 +580,7 @@ struct KaStage {
 };
 template <int DT>
 struct KaRaw {                                           // a wave's share of a page on its way
-  typedef KaCodes<1>::Words Words;
-  Words k[KaStage<DT>::KT / 4], v[KaStage<DT>::VT / 4];
+  KaWords k[KaStage<DT>::KT / 4], v[KaStage<DT>::VT / 4];
   float scale;
 };
 
@@ -567,13 +592,13 @@ __device__ __forceinline__ void ka_fetch(const unsigned char* head, int U, int w
     const int j = 4 * i + wave;                          // piece: 16 tokens x 4 groups of channels (DT = 64: 32 tokens x 2)
     const int tok = DT == 64 ? 32 * j + 16 * (g >> 1) + n : DT == 128 ? 16 * j + n : 16 * (j >> 1) + n;
     const int u = min(DT == 64 ? g & 1 : DT == 128 ? g : 4 * (j & 1) + g, U - 1);
-    raw.k[i] = *reinterpret_cast<const typename KaRaw<DT>::Words*>(head + (u32)(tok * U + u) * 12);
+    raw.k[i] = *reinterpret_cast<const KaWords*>(head + (u32)(tok * U + u) * 12);
   }
   const unsigned char* v = head + kp_code_bytes(U);
 #pragma unroll
   for (int i = 0; i < KaStage<DT>::VT / 4; ++i) {
     const int ch = min(16 * (4 * i + wave), 32 * U - 16) + n;
-    raw.v[i] = *reinterpret_cast<const typename KaRaw<DT>::Words*>(v + (u32)(ch * 4 + g) * 12);
+    raw.v[i] = *reinterpret_cast<const KaWords*>(v + (u32)(ch * 4 + g) * 12);
   }
   raw.scale = reinterpret_cast<const float*>(head + kp_scale_off(U))[threadIdx.x];       // waves 0, 1: keys; 2, 3: values
 }
@@ -624,7 +649,10 @@ __device__ __forceinline__ void ka_staged(const KaArgs& p, const KaRange& rg, in
     const uint4 w = digits[64 * j];
     dg[4 * j] = w.x; dg[4 * j + 1] = w.y; dg[4 * j + 2] = w.z; dg[4 * j + 3] = w.w;
   }
-  auto digit = [&](int i, int s, int d) -> const u32 (&)[6] { return *reinterpret_cast<const u32 (*)[6]>(dg + ((i * KS + s) * PARTS + d) * 6); };
+  auto digit = [&](int i, int s, int d) {
+    const u32* w = dg + ((i * KS + s) * PARTS + d) * 6;
+    return (v8i){(int)w[0], (int)w[1], (int)w[2], (int)w[3], (int)w[4], (int)w[5], 0, 0};
+  };
   v4f S[QT][8];
   auto key = [&](int j) { return DT == 64 ? sg.keys[32 * j + 16 * (g & 1) + n] : sg.keys[j * 64 + lane]; };
   uint4 ahead = key(0);
@@ -667,10 +695,16 @@ __device__ __forceinline__ void ka_staged(const KaArgs& p, const KaRange& rg, in
   auto scales = [&](int t) { return *reinterpret_cast<const float4*>(sg.vs + 16 * g + ka_token(t, 0)); };
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
-    if (masked) ka_mask(S[i], KaSeen(p, t0, qp[i], qp[i], 16 * g));
-    const float base = ka_rescale<DT>(S[i], qc[i], st[i]);
+    if (masked) ka_mask<1>(S[i], KaSeen(p, t0, qp[i], qp[i], 16 * g));
+    const float base = ka_rescale<DT, 16>(S[i], qc[i], st[i]);
     __builtin_amdgcn_sched_barrier(0);
-    ka_weights(S[i], scales, qc[i], base, st[i].l, ph[i], pl[i]);
+    int wh[8], wl[8];
+    ka_weights(S[i], scales, qc[i], base, st[i].l, wh, wl);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      ph[i][t] = wh[t];
+      pl[i][t] = wl[t];
+    }
     asm volatile("" : "+v"(ph[i]), "+v"(pl[i]), "+v"(st[i].l));      // (done here, not where it is used)
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -738,7 +772,7 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attention_rows_kernel(KaArgs
       qc[i] = qy.c;
       qp[i] = qy.pos;
 #pragma unroll
-      for (int e = 0; e < WORDS / QT; ++e) w[i * (WORDS / QT) + e] = (&qy.op[0][0][0])[e];
+      for (int e = 0; e < WORDS / QT; ++e) w[i * (WORDS / QT) + e] = (u32)qy.op[e / 6 / Query::PARTS][e / 6 % Query::PARTS][e % 6];
       st[i].clear();
     }
 #pragma unroll
@@ -754,7 +788,7 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attention_rows_kernel(KaArgs
     ka_widen<DT>(p, all, page, wave, raw, stage[0]);
   }
   __syncthreads();
-  auto turn = [&](auto first) {
+  auto turn = [&](auto first) __attribute__((always_inline)) {
     int page2 = 0;
     ++k;
     const unsigned char* next = ka_next(p, q, all, h, hb, 1, k, page2);
@@ -780,34 +814,46 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attention_rows_kernel(KaArgs
 }
 
 // Few rows: the pages are dealt to the four waves of `splits` workgroups; waves join in LDS, workgroups in the kernel below.
-// Partial results of (tile, head, split): 16 rows x (log2 maximum, sum), then 16 x DT outputs.
-__host__ __device__ static inline int64_t ka_part_floats(int DT) { return 16 * (DT + 2); }
+// Partial results of (tile, head, split): R rows x (log2 maximum, sum), then R x DT outputs.
+__host__ __device__ static inline int64_t ka_part_floats(int DT, int R) { return R * (DT + 2); }
 
-template <int DT, bool Q4, bool QV>
+template <int DT, int R, bool Q4, bool QV>
 __global__ __launch_bounds__(KA_THREADS, DT == 256 ? 1 : 2) void kv_attention_split_kernel(KaArgs p) {
-  __shared__ float lds_o[KA_WAVES - 1][16][DT + 4];
-  __shared__ float lds_m[KA_WAVES][16], lds_l[KA_WAVES][16];
+  constexpr int SHIFT = R == 16 ? 4 : R == 8 ? 3 : 2;
+  __shared__ float lds_o[KA_WAVES - 1][R][DT + 4];
+  __shared__ float lds_m[KA_WAVES][R], lds_l[KA_WAVES][R];
   const int h = (int)(blockIdx.x % (unsigned)p.H);
   const unsigned rest = blockIdx.x / (unsigned)p.H;
   const int split = (int)(rest % (unsigned)p.splits);
   const int64_t item = rest / (unsigned)p.splits;
   KvSeq q;
-  const int64_t local = kp_find(p.b, item, p.G, 4, 1, q);
+  const int64_t local = kp_find(p.b, item, p.G, SHIFT, 1, q);
   if (local < 0) return;                   // (whole workgroup)
   const int rows = q.n * p.G;
-  if ((local << 4) >= rows) return;
-  const int r0 = (int)(local << 4), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  if ((local << SHIFT) >= rows) return;
+  const int r0 = (int)(local << SHIFT), lane = threadIdx.x & 63, n = lane & (R - 1), g = lane >> 4;
+  const bool mine = (lane & 15) < R;       // one of a query's columns writes
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  KaQuery<DT, Q4, QV> qy[1];
-  KaState<DT> st[1];
-  qy[0].load(p, q, r0 + n, rows, h);
-  st[0].clear();
-  ka_walk<DT, Q4, QV>(p, q, ka_range(p, q, r0, 16, rows), h, split * KA_WAVES + wave, p.splits * KA_WAVES, qy[0], st[0]);
-  float l = st[0].l;
+  KaQuery<DT, Q4, QV> qy;
+  KaState<DT> st;
+  qy.load(p, q, r0 + n, rows, h);
+  st.clear();
+  ka_walk<DT, R, Q4, QV>(p, q, ka_range(p, q, r0, R, rows), h, split * KA_WAVES + wave, p.splits * KA_WAVES, qy, st);
+  // a query's columns together
+  auto columns = [](float v) {
+    if (R <= 8) v += ka_ror<8>(v);
+    if (R <= 4) v += ka_ror<4>(v);
+    return v;
+  };
+  float l = columns(st.l);
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
-  const float m = st[0].m == -INFINITY ? -INFINITY : st[0].m * qy[0].c;     // log2 units
-  if (g == 0) {
+#pragma unroll
+  for (int d = 0; d < DT / 16; ++d)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) st.o[d][e] = columns(st.o[d][e]);
+  const float m = st.m == -INFINITY ? -INFINITY : st.m * qy.c;     // log2 units
+  if (lane < R) {
     lds_m[wave][n] = m;
     lds_l[wave][n] = l;
   }
@@ -816,15 +862,15 @@ __global__ __launch_bounds__(KA_THREADS, DT == 256 ? 1 : 2) void kv_attention_sp
 #pragma unroll
   for (int w = 1; w < KA_WAVES; ++w) top = fmaxf(top, lds_m[w][n]);
   const float base = top == -INFINITY ? 0.0f : top;
-  const float mine = __builtin_amdgcn_exp2f(m - base);
-  if (wave > 0) {
+  const float f = __builtin_amdgcn_exp2f(m - base);
+  if (wave > 0 && mine) {
 #pragma unroll
     for (int d = 0; d < DT / 16; ++d)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) lds_o[wave - 1][n][16 * d + 4 * g + e] = st[0].o[d][e] * mine;
+      for (int e = 0; e < 4; ++e) lds_o[wave - 1][n][16 * d + 4 * g + e] = st.o[d][e] * f;
   }
   __syncthreads();
-  if (wave > 0) return;
+  if (wave > 0 || !mine || r0 + n >= rows) return;
   float sum = 0.0f;
 #pragma unroll
   for (int w = 0; w < KA_WAVES; ++w) sum += lds_l[w][n] * __builtin_amdgcn_exp2f(lds_m[w][n] - base);
@@ -832,50 +878,53 @@ __global__ __launch_bounds__(KA_THREADS, DT == 256 ? 1 : 2) void kv_attention_sp
   for (int d = 0; d < DT / 16; ++d)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      float v = st[0].o[d][e] * mine;
+      float v = st.o[d][e] * f;
 #pragma unroll
       for (int w = 0; w < KA_WAVES - 1; ++w) v += lds_o[w][n][16 * d + 4 * g + e];
-      st[0].o[d][e] = v;
+      st.o[d][e] = v;
     }
   if (p.splits == 1) {
-    if (r0 + n < rows) ka_store<DT>(p, q, r0 + n, h, st[0].o, sum > 0.0f ? 2.0f / sum : 0.0f);
+    ka_store<DT>(p, q, r0 + n, h, st.o, sum > 0.0f ? 2.0f / sum : 0.0f);
     return;
   }
-  float* part = p.part + ((item * p.H + h) * p.splits + split) * ka_part_floats(DT);
-  if (r0 + n >= rows) return;
+  float* part = p.part + ((item * p.H + h) * p.splits + split) * ka_part_floats(DT, R);
   if (g == 0) {
     part[n] = top;
-    part[16 + n] = sum;
+    part[R + n] = sum;
   }
 #pragma unroll
-  for (int d = 0; d < DT / 16; ++d) *reinterpret_cast<v4f*>(part + 32 + n * DT + 16 * d + 4 * g) = st[0].o[d];
+  for (int d = 0; d < DT / 16; ++d)
+#pragma unroll
+    for (int e = 0; e < 4; e += 2)
+      *reinterpret_cast<float2*>(part + 2 * R + n * DT + 16 * d + 4 * g + e) = make_float2(st.o[d][e], st.o[d][e + 1]);
 }
 
 // Joins the workgroups' partial results: a workgroup has one row of a tile and head, its waves a quarter of the splits each.
 template <int DT>
-__global__ __launch_bounds__(KA_THREADS) void kv_attention_join_kernel(KaArgs p) {
+__global__ __launch_bounds__(KA_THREADS) void kv_attention_join_kernel(KaArgs p, int shift) {
   constexpr int PER = DT / 64;             // channels a lane
   __shared__ float lds_o[KA_WAVES][DT];
-  const int n = (int)(blockIdx.x & 15u);
-  const unsigned rest = blockIdx.x >> 4;
+  const int R = 1 << shift, n = (int)(blockIdx.x & (unsigned)(R - 1));
+  const unsigned rest = blockIdx.x >> shift;
   const int h = (int)(rest % (unsigned)p.H);
   const int64_t item = rest / (unsigned)p.H;
   KvSeq q;
-  const int64_t local = kp_find(p.b, item, p.G, 4, 1, q);
+  const int64_t local = kp_find(p.b, item, p.G, shift, 1, q);
   if (local < 0) return;
   const int rows = q.n * p.G;
-  if ((local << 4) + n >= rows) return;    // (whole workgroup)
-  const float* part = p.part + (item * p.H + h) * p.splits * ka_part_floats(DT);
+  if ((local << shift) + n >= rows) return;    // (whole workgroup)
+  const int64_t stride = ka_part_floats(DT, R);
+  const float* part = p.part + (item * p.H + h) * p.splits * stride;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // every wave has all maxima and sums
   float top = -INFINITY;
-  for (int s = lane; s < p.splits; s += 64) top = fmaxf(top, part[s * ka_part_floats(DT) + n]);
+  for (int s = lane; s < p.splits; s += 64) top = fmaxf(top, part[s * stride + n]);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
   const float base = top == -INFINITY ? 0.0f : top;
   float sum = 0.0f;
   for (int s = lane; s < p.splits; s += 64)
-    sum += part[s * ka_part_floats(DT) + 16 + n] * __builtin_amdgcn_exp2f(part[s * ka_part_floats(DT) + n] - base);
+    sum += part[s * stride + R + n] * __builtin_amdgcn_exp2f(part[s * stride + n] - base);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
   float acc[PER];
@@ -883,10 +932,10 @@ __global__ __launch_bounds__(KA_THREADS) void kv_attention_join_kernel(KaArgs p)
   for (int e = 0; e < PER; ++e) acc[e] = 0.0f;
 #pragma unroll 4
   for (int s = wave; s < p.splits; s += KA_WAVES) {
-    const float* ps = part + s * ka_part_floats(DT);
+    const float* ps = part + s * stride;
     const float f = __builtin_amdgcn_exp2f(ps[n] - base);
 #pragma unroll
-    for (int e = 0; e < PER; ++e) acc[e] = __builtin_fmaf(ps[32 + n * DT + PER * lane + e], f, acc[e]);
+    for (int e = 0; e < PER; ++e) acc[e] = __builtin_fmaf(ps[2 * R + n * DT + PER * lane + e], f, acc[e]);
   }
 #pragma unroll
   for (int e = 0; e < PER; ++e) lds_o[wave][PER * lane + e] = acc[e];
@@ -897,7 +946,7 @@ __global__ __launch_bounds__(KA_THREADS) void kv_attention_join_kernel(KaArgs p)
   float v[2];
 #pragma unroll
   for (int e = 0; e < 2; ++e) v[e] = (((lds_o[0][c + e] + lds_o[1][c + e]) + lds_o[2][c + e]) + lds_o[3][c + e]) * inv;
-  const int r = (int)(local << 4) + n, i = r / p.G;
+  const int r = (int)(local << shift) + n, i = r / p.G;
   uint16_t* out = p.O + ((int64_t)(q.q0 + i) * p.Hq + h * p.G + (r - i * p.G)) * p.D;
   *reinterpret_cast<u32*>(out + c) = bl_pack_bf16(v[0], v[1]);
 }
@@ -907,18 +956,24 @@ __global__ __launch_bounds__(KA_THREADS) void kv_attention_join_kernel(KaArgs p)
 static int64_t ka_tiles(int64_t T, int64_t G, int64_t n_seqs, int shift) { return ((T * G) >> shift) + n_seqs; }
 static int ka_dt(int64_t D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
-// Workgroups along the keys; 0: the rows fill the chip without
-static int ka_splits(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t max_pages) {
-  const int64_t tiles = ka_tiles(T, G, n_seqs, 4) * H;
-  if (tiles >= 2048) return 0;
+// How a call is dealt out: `splits` workgroups along the keys for tiles of 2^shift rows, or (0) whole rows
+struct KaPlan {
+  int splits, shift;
+};
+static KaPlan ka_plan(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t max_pages) {
+  const int64_t full = ka_tiles(T, G, n_seqs, 4) * H;
+  if (full >= 2048) return {0, 0};
+  // rows a sequence: tiles of 4 or 8 do without the softmax of empty columns
+  const int shift = T * G <= 4 * n_seqs ? 2 : T * G <= 8 * n_seqs ? 3 : 4;
+  const int64_t tiles = ka_tiles(T, G, n_seqs, shift) * H;
   const int64_t want = (512 + tiles - 1) / tiles, most = (max_pages + KA_WAVES - 1) / KA_WAVES;
-  return (int)(want < most ? want : most);
+  return {(int)(want < most ? want : most), shift};
 }
 
 size_t bl_kv_attention_ws_bytes(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t D, int64_t max_pages) {
-  const int splits = ka_splits(T, n_seqs, G, H, max_pages);
-  if (splits <= 1) return 0;
-  return (size_t)(ka_tiles(T, G, n_seqs, 4) * H * splits * ka_part_floats(ka_dt(D)) * 4);
+  const KaPlan k = ka_plan(T, n_seqs, G, H, max_pages);
+  if (k.splits <= 1) return 0;
+  return (size_t)(ka_tiles(T, G, n_seqs, k.shift) * H * k.splits * ka_part_floats(ka_dt(D), 1 << k.shift) * 4);
 }
 
 int bl_launch_kv_attention(const void* Q, int64_t ldq, bl_dtype qdt, int Hq, int H, int D, int q_bits, const KvBatch& b,
@@ -934,12 +989,15 @@ int bl_launch_kv_attention(const void* Q, int64_t ldq, bl_dtype qdt, int Hq, int
   p.sinks = (int)(sinks < 0x7FFFFF00 ? sinks : 0x7FFFFF00);
   p.pages = (const unsigned char*)pages;
   p.O = (uint16_t*)O; p.part = (float*)ws;
-  p.splits = ka_splits(b.T, b.n_seqs, p.G, H, b.max_pages);
+  const KaPlan plan = ka_plan(b.T, b.n_seqs, p.G, H, b.max_pages);
+  p.splits = plan.splits;
   const int dt = ka_dt(D);
   const bool qv = qdt == BL_BF16 && D % 32 == 0 && bl_aligned16(Q) && ldq % 8 == 0 && bl_aligned16(rope);
 #define KA_GO2(DT, Q4, QV)                                                                               \
   do {                                                                                                   \
-    if (p.splits) kv_attention_split_kernel<DT, Q4, QV><<<blocks, KA_THREADS, 0, s>>>(p);                \
+    if (p.splits && shift == 2) kv_attention_split_kernel<DT, 4, Q4, QV><<<blocks, KA_THREADS, 0, s>>>(p); \
+    else if (p.splits && shift == 3) kv_attention_split_kernel<DT, 8, Q4, QV><<<blocks, KA_THREADS, 0, s>>>(p); \
+    else if (p.splits) kv_attention_split_kernel<DT, 16, Q4, QV><<<blocks, KA_THREADS, 0, s>>>(p);       \
     else {                                                                                               \
       constexpr int lds = (int)(2 * sizeof(KaStage<DT>)) + KA_WAVES * 64 * 4 * KA_QT(DT) * KaQuery<DT, Q4, QV>::WORDS; \
       BL_SET_MAX_LDS_ONCE((kv_attention_rows_kernel<DT, KA_QT(DT), Q4, QV>), lds);                       \
@@ -954,7 +1012,7 @@ int bl_launch_kv_attention(const void* Q, int64_t ldq, bl_dtype qdt, int Hq, int
       if (qv) KA_GO2(DT, false, true); else KA_GO2(DT, false, false); \
     }                                                              \
   } while (0)
-  const int shift = p.splits ? 4 : 6 + (KA_QT(dt) == 2);           // four waves of KA_QT tiles of 16 rows
+  const int shift = p.splits ? plan.shift : 6 + (KA_QT(dt) == 2);           // four waves of KA_QT tiles of 16 rows
   const int64_t tiles = ka_tiles(b.T, p.G, b.n_seqs, shift);
   const int64_t n_blocks = tiles * H * (p.splits ? p.splits : 1);
   if (!bl_grid_ok(n_blocks) || !bl_grid_ok(tiles * H * 16)) return BL_ESHAPE;
@@ -962,10 +1020,10 @@ int bl_launch_kv_attention(const void* Q, int64_t ldq, bl_dtype qdt, int Hq, int
   if (dt == 64) KA_GO(64); else if (dt == 128) KA_GO(128); else KA_GO(256);
   BL_HIP_CHECK_LAUNCH();
   if (p.splits > 1) {
-    const unsigned joins = (unsigned)(tiles * H * 16);
-    if (dt == 64) kv_attention_join_kernel<64><<<joins, KA_THREADS, 0, s>>>(p);
-    else if (dt == 128) kv_attention_join_kernel<128><<<joins, KA_THREADS, 0, s>>>(p);
-    else kv_attention_join_kernel<256><<<joins, KA_THREADS, 0, s>>>(p);
+    const unsigned joins = (unsigned)((tiles * H) << shift);
+    if (dt == 64) kv_attention_join_kernel<64><<<joins, KA_THREADS, 0, s>>>(p, shift);
+    else if (dt == 128) kv_attention_join_kernel<128><<<joins, KA_THREADS, 0, s>>>(p, shift);
+    else kv_attention_join_kernel<256><<<joins, KA_THREADS, 0, s>>>(p, shift);
     BL_HIP_CHECK_LAUNCH();
   }
 #undef KA_GO

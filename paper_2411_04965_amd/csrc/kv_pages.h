@@ -31,6 +31,12 @@ struct KvSeq {
   int64_t len, pos0;             // length with the new tokens, position of the first of them (negative if n > len)
 };
 
+// A batch's numbers at a place that is the same for a whole wave, through the scalar cache (nothing writes them while a kernel runs).
+// As vector loads they would be waited for behind everything a wave has on its way: loads come back in order.
+__device__ __forceinline__ int kp_scalar(const int32_t* p, int64_t i) {
+  return ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)p)[i];
+}
+
 // Work items are dealt to sequences without the host knowing their lengths: sequence s owns the items from
 // floor(q_start[s] * mul / 2^shift) + per * s on.  That start grows by at least floor(rows * mul / 2^shift) + per, so every
 // sequence has enough items and the total is known on the host.
@@ -54,21 +60,25 @@ __device__ __forceinline__ int64_t kp_find(const KvBatch& b, int64_t item, int m
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
   q.s = lo;
-  q.q0 = min(max(b.q_start[lo], 0), b.T);
-  q.n = min(max(b.q_start[lo + 1], 0), b.T) - q.q0;
-  q.len = b.kv_len[lo];
+  q.q0 = min(max(kp_scalar(b.q_start, lo), 0), b.T);
+  q.n = min(max(kp_scalar(b.q_start, lo + 1), 0), b.T) - q.q0;
+  q.len = kp_scalar(b.kv_len, lo);
   q.pos0 = q.len - q.n;
-  const int64_t local = item - kp_first_item(b, lo, mul, shift, per);
+  const int64_t local = item - ((((int64_t)q.q0 * mul) >> shift) + (int64_t)per * lo);
   return q.n > 0 && local >= 0 ? local : -1;
 }
 
 // Words A, B, C of 32 codes -> 32 E2M1 nibbles (code i in nibble i % 8 of word i / 8).  A code's two magnitude bits m are the
-// nibble of the value m / 2, so nothing but shifts and masks is needed: 13 instructions for 32 codes.
+// nibble of the value m / 2, so nothing but shifts and masks is needed: 11 instructions for 32 codes (a sign word cleared of the
+// bits between, then one bit-wise choice a nibble word).
 __device__ __forceinline__ void kp_expand(u32 A, u32 B, u32 C, u32 (&o)[4]) {
-  o[0] = (A & 0x33333333u) | (C & 0x88888888u);
-  o[1] = ((A >> 2) & 0x33333333u) | ((C << 1) & 0x88888888u);
-  o[2] = (B & 0x33333333u) | ((C << 2) & 0x88888888u);
-  o[3] = ((B >> 2) & 0x33333333u) | ((C << 3) & 0x88888888u);
+  u32 even = C & 0xAAAAAAAAu, odd = (C << 1) & 0xAAAAAAAAu;
+  asm("" : "+v"(even), "+v"(odd));                     // (known bits would turn the choices back into two instructions each)
+  auto choose = [](u32 mag, u32 sign) { return (mag & 0x33333333u) | (sign & 0xCCCCCCCCu); };
+  o[0] = choose(A, even);
+  o[1] = choose(A >> 2, odd);
+  o[2] = choose(B, even << 2);
+  o[3] = choose(B >> 2, odd << 2);
 }
 // bit of code i in C and in a word of lowest magnitude bits
 __host__ __device__ __forceinline__ int kp_sign_bit(int i) { return 4 * (i & 7) + 3 - (i >> 3); }

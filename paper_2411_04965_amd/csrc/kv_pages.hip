@@ -75,7 +75,7 @@ __global__ __launch_bounds__(KP_THREADS) void kv_append_kernel(
   if (local < 0) return;
   const int64_t pg = (q.pos0 > 0 ? q.pos0 >> 7 : 0) + local;
   if (pg >= b.max_pages || pg * KP_TOKENS >= q.len) return;
-  const int id = b.table[(int64_t)q.s * b.max_pages + pg];
+  const int id = kp_scalar(b.table, (int64_t)q.s * b.max_pages + pg);
   if (id < 0 || id >= b.n_pages) return;
   // tokens a .. e - 1 of the page are new
   const int a = (int)max(q.pos0 - pg * KP_TOKENS, (int64_t)0), e = (int)min(q.len - pg * KP_TOKENS, (int64_t)KP_TOKENS);
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(KP_THREADS) void kv_read_kernel(const unsigned char
   if (local < 0) return;
   const int64_t pg = (q.pos0 > 0 ? q.pos0 >> 7 : 0) + local;
   if (pg >= b.max_pages || pg * KP_TOKENS >= q.len) return;
-  const int id = b.table[(int64_t)q.s * b.max_pages + pg];
+  const int id = kp_scalar(b.table, (int64_t)q.s * b.max_pages + pg);
   if (id < 0 || id >= b.n_pages) return;
   const int a = (int)max(q.pos0 - pg * KP_TOKENS, (int64_t)0), e = (int)min(q.len - pg * KP_TOKENS, (int64_t)KP_TOKENS);
   const int U = kp_units(D);
