@@ -42,6 +42,7 @@ struct KaArgs {
   uint16_t* O;
   float* part;                            // partial results of split rows (ka_part_floats)
   int splits;
+  int slots;                              // items a sequence, where all have as many (order below); else 1
 };
 
 __device__ __forceinline__ v4f ka_mfma_pv(const u32 (&a)[4], v8i b, v4f c, int sa, int sb) {
@@ -817,6 +818,13 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attention_rows_kernel(KaArgs
 // Partial results of (tile, head, split): R rows x (log2 maximum, sum), then R x DT outputs.
 __host__ __device__ static inline int64_t ka_part_floats(int DT, int R) { return R * (DT + 2); }
 
+// A decoding batch has one item with rows and one without for every sequence, in turn, and an XCD deals workgroups to its shader
+// engines in turn as well: half of them got the empty ones (64 sequences x 8 heads: 32 of an XCD's 64 workgroups ran on 16 CUs, 77 us).
+// Where every sequence has as many items, all first ones go before all second ones.
+__device__ __forceinline__ int64_t ka_item(const KaArgs& p, unsigned i) {
+  return p.slots > 1 ? (int64_t)(i % (unsigned)p.b.n_seqs) * p.slots + i / (unsigned)p.b.n_seqs : (int64_t)i;
+}
+
 template <int DT, int R, bool Q4, bool QV>
 __global__ __launch_bounds__(KA_THREADS, DT == 256 ? 1 : 2) void kv_attention_split_kernel(KaArgs p) {
   constexpr int SHIFT = R == 16 ? 4 : R == 8 ? 3 : 2;
@@ -825,7 +833,7 @@ __global__ __launch_bounds__(KA_THREADS, DT == 256 ? 1 : 2) void kv_attention_sp
   const int h = (int)(blockIdx.x % (unsigned)p.H);
   const unsigned rest = blockIdx.x / (unsigned)p.H;
   const int split = (int)(rest % (unsigned)p.splits);
-  const int64_t item = rest / (unsigned)p.splits;
+  const int64_t item = ka_item(p, rest / (unsigned)p.splits);
   KvSeq q;
   const int64_t local = kp_find(p.b, item, p.G, SHIFT, 1, q);
   if (local < 0) return;                   // (whole workgroup)
@@ -961,8 +969,10 @@ struct KaPlan {
   int splits, shift;
 };
 static KaPlan ka_plan(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t max_pages) {
-  const int64_t full = ka_tiles(T, G, n_seqs, 4) * H;
-  if (full >= 2048) return {0, 0};
+  // Whole rows where there are enough of them for the workgroups of 128 (or 64) rows to be filled and to fill the chip: 1000 rows x 32
+  // heads of 64 channels without a cache 37 us, 56 split; 64 sequences x 16 rows x 8 heads, 2000 cached: 95 and 37; a chunk of 500 among
+  // 15 single tokens x 32 heads: 75 and 55.
+  if (T * G >= 64 * n_seqs && ka_tiles(T, G, n_seqs, 4) * H >= 512) return {0, 0};
   // rows a sequence: tiles of 4 or 8 do without the softmax of empty columns
   const int shift = T * G <= 4 * n_seqs ? 2 : T * G <= 8 * n_seqs ? 3 : 4;
   const int64_t tiles = ka_tiles(T, G, n_seqs, shift) * H;
@@ -1015,6 +1025,7 @@ int bl_launch_kv_attention(const void* Q, int64_t ldq, bl_dtype qdt, int Hq, int
   const int shift = p.splits ? plan.shift : 6 + (KA_QT(dt) == 2);           // four waves of KA_QT tiles of 16 rows
   const int64_t tiles = ka_tiles(b.T, p.G, b.n_seqs, shift);
   const int64_t n_blocks = tiles * H * (p.splits ? p.splits : 1);
+  p.slots = tiles % b.n_seqs == 0 ? (int)(tiles / b.n_seqs) : 1;
   if (!bl_grid_ok(n_blocks) || !bl_grid_ok(tiles * H * 16)) return BL_ESHAPE;
   const unsigned blocks = (unsigned)n_blocks;
   if (dt == 64) KA_GO(64); else if (dt == 128) KA_GO(128); else KA_GO(256);
