@@ -10,6 +10,8 @@
 
 #define KP_THREADS 256
 
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
 template <typename RawT>
 __device__ __forceinline__ float kp_to_f32(RawT v) {
   return sizeof(RawT) == 2 ? __uint_as_float((u32)v << 16) : __uint_as_float((u32)v);
@@ -86,6 +88,22 @@ __global__ __launch_bounds__(KP_THREADS) void kv_append_kernel(
   u32* lows = reinterpret_cast<u32*>(head + kp_low_off(U));
   const int j = threadIdx.x % LPT, c = 8 * j, jq = j & 3, u = j >> 2;
 
+  // older tokens' bits in the value words that this thread will put together: on their way before anything else
+  constexpr int ITEMS = ROW * 4 / KP_THREADS;
+  u32 old[ITEMS][3];
+  u32* const v_words = reinterpret_cast<u32*>(head + kp_code_bytes(U));
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    const int it = (int)threadIdx.x + k * KP_THREADS, gr = it / Dp, d = it - gr * Dp;
+    const int lo = max(a - 32 * gr, 0), hi = min(e - 32 * gr, 32);
+    if (it < 4 * Dp && lo < hi && hi - lo < 32) {
+#pragma unroll
+      for (int i = 0; i < 3; ++i) old[k][i] = v_words[(d * 4 + gr) * 3 + i];
+    } else {
+      old[k][0] = old[k][1] = old[k][2] = 0u;
+    }
+  }
+
   for (int base = a; base < e; base += KP_THREADS / LPT) {      // (every lane stays: the quads exchange words)
     const int tok = base + (int)threadIdx.x / LPT;
     const bool have = tok < e;
@@ -93,18 +111,36 @@ __global__ __launch_bounds__(KP_THREADS) void kv_append_kernel(
     const int64_t row = have ? q.q0 + (pos - q.pos0) : q.q0;
     const bool four = pos == 0;
     const float qb = four ? 7.0f : 3.0f;
-    float v[8];
+    float v[8], y[8];
     u32 lv[8];
-    // key
+    // key and value
     const RawT* x = K + row * ldk + (int64_t)h * D;
     kp_load8<RawT, VEC>(x, c, D, v);
+    kp_load8<RawT, VEC>(V + row * ldv + (int64_t)h * D, c, D, y);
     if (rope) {
       const float* rr = rope + min(pos, n_pos - 1) * D;
-      float o[8];
       if (VEC) {
-        kp_load8<RawT, true>(x, c < half ? c + half : c - half, D, o);
+        // 8 channels lie in one half of the pairs; the first half subtracts (kp_rotate's steps)
+        float o[8], cs[8], sn[8];
+        const int cc = min(c, D - 8), pair = cc < half ? cc : cc - half;
+        kp_load8<RawT, true>(x, cc < half ? cc + half : cc - half, D, o);
+        const f32x4_any* cp = reinterpret_cast<const f32x4_any*>(rr + pair);
+        const f32x4_any* sp = reinterpret_cast<const f32x4_any*>(rr + half + pair);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (c < D) v[i] = kp_rotate(v[i], o[i], rr, c + i, half);
+        for (int i = 0; i < 2; ++i) {
+          const f32x4_any c4 = cp[i], s4 = sp[i];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            cs[4 * i + k] = c4[k];
+            sn[4 * i + k] = s4[k];
+          }
+        }
+        const u32 flip = cc < half ? 0x80000000u : 0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float r = v[i] * cs[i] + __uint_as_float(__float_as_uint(o[i]) ^ flip) * sn[i];
+          v[i] = c < D ? r : 0.0f;
+        }
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -136,10 +172,8 @@ __global__ __launch_bounds__(KP_THREADS) void kv_append_kernel(
       if (jq < 3) w[jq] = jq == 0 ? mag : jq == 1 ? magB : sgn;
       if (four && jq == 3) lows[u] = low;
     }
-    // value
-    kp_load8<RawT, VEC>(V + row * ldv + (int64_t)h * D, c, D, v);
-    g = kp_head_max<LPT>(v);
-    kp_levels8(v, qb / (g + eps), qb, four, lv);
+    g = kp_head_max<LPT>(y);
+    kp_levels8(y, qb / (g + eps), qb, four, lv);
     if (have) {
       if (j == 0) v_scale[tok] = g / qb;
       uint2 w = make_uint2(0u, 0u);
@@ -158,11 +192,12 @@ __global__ __launch_bounds__(KP_THREADS) void kv_append_kernel(
     for (int i = 0; i < 32; ++i) w |= (u32)((vq[32 * threadIdx.x + i] >> 3) & 1) << kp_sign_bit(i);
     lows[U + threadIdx.x] = w;
   }
-  for (int it = threadIdx.x; it < 4 * Dp; it += KP_THREADS) {
-    const int g = it / Dp, d = it - g * Dp;
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    const int it = (int)threadIdx.x + k * KP_THREADS, g = it / Dp, d = it - g * Dp;
     const int lo = max(a - 32 * g, 0), hi = min(e - 32 * g, 32);            // tokens lo .. hi - 1 of the 32
-    if (lo >= hi) continue;
-    u32* w = reinterpret_cast<u32*>(head + kp_code_bytes(U)) + (d * 4 + g) * 3;
+    if (it >= 4 * Dp || lo >= hi) continue;
+    u32* w = v_words + (d * 4 + g) * 3;
     u32 nw[3] = {0u, 0u, 0u}, keep[3] = {~0u, ~0u, ~0u};
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
@@ -175,8 +210,8 @@ __global__ __launch_bounds__(KP_THREADS) void kv_append_kernel(
       }
     }
 #pragma unroll
-    for (int k = 0; k < 3; ++k)
-      if (keep[k] != ~0u) w[k] = keep[k] ? (w[k] & keep[k]) | nw[k] : nw[k];
+    for (int i = 0; i < 3; ++i)
+      if (keep[i] != ~0u) w[i] = (old[k][i] & keep[i]) | nw[i];
   }
 }
 
