@@ -11,12 +11,13 @@
 // of the largest channel.  6-bit x 4-bit products take half the time of 8-bit x 4-bit ones: three of them 51 cycles, two E4M3 parts (8
 // significand bits of every channel) 66.  4-bit queries (absmax, 7 levels) are one digit.
 //   Probabilities, times the value's scale, need relative precision: each is the sum of two E4M3 numbers, the second scaled by 2^-5,
-// which is one rounding to 8 significand bits, as bfloat16 operands would have it.
+// which is one rounding to 8 significand bits, as bfloat16 operands would have it.  (Where many rows share a page the values widen to
+// bfloat16 and the probabilities are rounded to that instead.)
 // Products are exact, sums float32.
 //
 // Keys are the row operand, queries the column operand: a lane ends up with the scores of one query against 4 consecutive tokens
 // of every 16, which is, byte for byte, the eight-bit column operand of the second product (kp_slot: keys are stored in the order
-// that makes it so).  Scores and probabilities never leave the lane but for two maxima a page; nothing goes through LDS.
+// that makes it so).  Scores and probabilities never leave the lane but for their maxima.
 //
 // The first token has 4 bits, level = sign (2 mag + low): its scale is doubled, and one more instruction with the low bits in
 // place of the codes and the scale operand 1/2 adds the rest, in the sequence's first page only.
@@ -24,7 +25,6 @@
 
 #define KA_THREADS 256
 #define KA_WAVES 4
-#define KA_QT(DT) ((DT) == 256 ? 1 : 2)      // tiles of 16 rows a wave where the rows fill the chip
 
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef short v2s __attribute__((ext_vector_type(2)));
@@ -79,8 +79,11 @@ template <int R = 16>
 __device__ __forceinline__ float ka_max_groups(float v) {
   if (R <= 8) v = fmaxf(v, ka_ror<8>(v));
   if (R <= 4) v = fmaxf(v, ka_ror<4>(v));
-  v = fmaxf(v, __shfl_xor(v, 16, 64));
-  return fmaxf(v, __shfl_xor(v, 32, 64));
+  // (both halves, then both rows of 16, of a copy exchanged: no trip through LDS)
+  auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+  x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
 }
 
 __device__ __forceinline__ float ka_q_at(const KaArgs& p, int64_t at) {
@@ -363,21 +366,34 @@ __device__ __forceinline__ void ka_mask(v4f (&S)[N], KaSeen see) {
     for (int r = 0; r < 4; ++r) S[t][r] = see.at(ka_token(STEP * t, r)) ? S[t][r] : -INFINITY;
 }
 
-// New maximum over a page's scores, what was summed so far brought to it; -> the maximum in log2 units
+// New maxima `mx` over a lane's scores of a page, what was summed so far brought to them; base: the maxima in log2 units
+template <int DT, int R, int N>
+__device__ __forceinline__ void ka_raise(const float* mx, const float* c, KaState<DT>* st, float* base) {
+  float m[N];
+  bool up = false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    m[i] = fmaxf(st[i].m, ka_max_groups<R>(mx[i]));
+    base[i] = m[i] == -INFINITY ? 0.0f : m[i] * c[i];      // nothing seen so far: all terms are exp2(-inf) = 0
+    up |= m[i] > st[i].m;
+  }
+  if (__any(up)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float al = __builtin_amdgcn_exp2f(st[i].m * c[i] - base[i]);
+      st[i].l *= al;
+#pragma unroll
+      for (int t = 0; t < DT / 16; ++t) st[i].o[t] *= al;
+      st[i].m = m[i];
+    }
+  }
+}
 template <int DT, int R, int N>
 __device__ __forceinline__ float ka_rescale(const v4f (&S)[N], float c, KaState<DT>& st) {
-  float mx = -INFINITY;
+  float mx = -INFINITY, base;
 #pragma unroll
   for (int t = 0; t < N; ++t) mx = ka_max3(ka_max3(mx, S[t][0], S[t][1]), S[t][2], S[t][3]);
-  const float m = fmaxf(st.m, ka_max_groups<R>(mx));
-  const float base = m == -INFINITY ? 0.0f : m * c;      // nothing seen so far: all terms are exp2(-inf) = 0
-  if (__any(m > st.m)) {
-    const float al = __builtin_amdgcn_exp2f(st.m * c - base);
-    st.l *= al;
-#pragma unroll
-    for (int t = 0; t < DT / 16; ++t) st.o[t] *= al;
-    st.m = m;
-  }
+  ka_raise<DT, R, 1>(&mx, &c, &st, &base);
   return base;
 }
 
@@ -567,13 +583,12 @@ __device__ __forceinline__ void ka_store(const KaArgs& p, const KvSeq& q, int r,
   }
 }
 
-// Many rows: a workgroup has 4 x QT x 16 rows (row = new token x query head of the group) of one key / value head and walks their
-// pages; each wave widens a quarter of a page's codes into LDS, where all four read them as operands, while the page before is worked
-// on.  That leaves a wave 13 registers for the page to come and a quarter of the widening, and its scales come prepared: a page costs a
-// wave of 32 rows about 650 vector instructions where a wave of its own pages takes 1060, which is what bounds this kernel.
+// Many rows, more than 128 channels: a workgroup has 4 x QT x 16 rows (row = new token x query head of the group) of one key / value
+// head and walks their pages; each wave widens a quarter of a page's codes into LDS, where all four read them as operands, while the
+// page before is worked on.  (The kernel below it, for up to 128 channels, keeps the values in bfloat16, for which LDS has no room here.)
 template <int DT>
 struct KaStage {
-  static constexpr int KT = DT == 64 ? 4 : DT / 16;      // 1 KB pieces of key operands (DT = 64: 16 tokens take half a one)
+  static constexpr int KT = DT / 16;                     // 1 KB pieces of key operands
   static constexpr int VT = DT / 16;                     // and of value operands
   uint4 keys[KT * 64], vals[VT * 64];
   float ks[KP_TOKENS], vs[KP_TOKENS];
@@ -590,9 +605,8 @@ __device__ __forceinline__ void ka_fetch(const unsigned char* head, int U, int w
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int i = 0; i < KaStage<DT>::KT / 4; ++i) {
-    const int j = 4 * i + wave;                          // piece: 16 tokens x 4 groups of channels (DT = 64: 32 tokens x 2)
-    const int tok = DT == 64 ? 32 * j + 16 * (g >> 1) + n : DT == 128 ? 16 * j + n : 16 * (j >> 1) + n;
-    const int u = min(DT == 64 ? g & 1 : DT == 128 ? g : 4 * (j & 1) + g, U - 1);
+    const int j = 4 * i + wave;                          // piece: 16 tokens x 4 groups of channels
+    const int tok = 16 * (j >> 1) + n, u = min(4 * (j & 1) + g, U - 1);
     raw.k[i] = *reinterpret_cast<const KaWords*>(head + (u32)(tok * U + u) * 12);
   }
   const unsigned char* v = head + kp_code_bytes(U);
@@ -655,7 +669,7 @@ __device__ __forceinline__ void ka_staged(const KaArgs& p, const KaRange& rg, in
     return (v8i){(int)w[0], (int)w[1], (int)w[2], (int)w[3], (int)w[4], (int)w[5], 0, 0};
   };
   v4f S[QT][8];
-  auto key = [&](int j) { return DT == 64 ? sg.keys[32 * j + 16 * (g & 1) + n] : sg.keys[j * 64 + lane]; };
+  auto key = [&](int j) { return sg.keys[j * 64 + lane]; };
   uint4 ahead = key(0);
 #pragma unroll
   for (int j = 0; j < 8 * KS; ++j) {
@@ -674,7 +688,7 @@ __device__ __forceinline__ void ka_staged(const KaArgs& p, const KaRange& rg, in
   if (FIRST) {                         // the first token's lowest bits (its scales are doubled in LDS)
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      const int u = min(DT == 64 ? g & 1 : 4 * s + g, U - 1);
+      const int u = min(4 * s + g, U - 1);
       u32 a[4];
       ka_low_keys(n == 0 ? lows[u] : 0u, n == 0 ? reinterpret_cast<const u32*>(head)[u * 3 + 2] : 0u, a);
 #pragma unroll
@@ -742,7 +756,7 @@ __device__ __forceinline__ void ka_staged(const KaArgs& p, const KaRange& rg, in
 }
 
 template <int DT, int QT, bool Q4, bool QV>
-__global__ __launch_bounds__(KA_THREADS, 2) void kv_attention_rows_kernel(KaArgs p, int shift, int n_tiles) {
+__global__ __launch_bounds__(KA_THREADS, 2) void kv_attention_wide_kernel(KaArgs p, int shift, int n_tiles) {
   extern __shared__ __align__(16) unsigned char ka_smem[];
   KaStage<DT>* stage = reinterpret_cast<KaStage<DT>*>(ka_smem);
   typedef KaQuery<DT, Q4, QV> Query;
@@ -804,6 +818,365 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attention_rows_kernel(KaArgs
   };
   if (head && page == 0) turn(std::true_type());
   while (head) turn(std::false_type());
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    float l = st[i].l;
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    const int r = r0 + 16 * i + n;
+    if (r < rows) ka_store<DT>(p, q, r, h, st[i].o, l > 0.0f ? 2.0f / l : 0.0f);
+  }
+}
+
+// Many rows, up to 128 channels: a workgroup has 8 x QT x 16 rows of one key / value head, one workgroup a CU.
+// The matrix and the vector unit take about as long for a page, so a wave's instructions for them are interleaved: in turn q the scores
+// of page q (made in the turn before) are scaled and their maximum found between the products of page q - 1's probabilities and values;
+// then they become probabilities tile by tile, and page q + 1's scores take the registers of a tile as it is used up.  What turn q's
+// products read is bundle q, the values of page q - 1 and the keys of page q + 1, in buffer q % 2; bundle q + 1 is widened into the
+// other buffer meanwhile, from codes that each wave fetched a turn ago.  One barrier a turn.  2048 rows x 32 heads of 128 on 6144 cached:
+// 254 us where calls follow each other (950 TFLOP/s of two products that would be bfloat16's), 290 with both products of a page behind
+// one another and four waves; 8800 clocks a page of 256 rows, of which the matrix unit is busy 3700 and the vector unit about 6000, and
+// the clock falls from 2.4 to 1.9 GHz: the vector unit's softmax and the power bound it.
+// Probabilities times the values' scales are bfloat16 here: the values widen to bfloat16 once for 8 x QT x 16 rows (levels / 2, the
+// first token's with its lowest bit, exact), and two conversions of the E4M3 pair that few rows take are saved for every score.
+#define KR_WAVES 8
+#define KR_THREADS (64 * KR_WAVES)
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+
+template <int DT>
+struct KrBundle {
+  uint4 keys[(DT == 64 ? 4 : 8) * 64];      // 16 tokens x 128 channels a KB (DT = 64: 32 tokens x 64)
+  uint4 vals[DT / 16 * 4 * 64];             // 16 channels x 32 tokens a KB, [channels][tokens]
+};
+struct KrScales {
+  float k[KP_TOKENS], v[KP_TOKENS];
+};
+struct KrRaw {                              // a wave's share of a bundle on its way
+  KaWords k, v;
+  float s;
+};
+template <int DT, int QT, bool Q4, bool QV>
+struct KrShared {
+  static constexpr int WORDS = (QT * KaQuery<DT, Q4, QV>::WORDS + 3) / 4 * 4;
+  KrBundle<DT> bundle[2];
+  KrScales scales[4];                       // page q in q % 4
+  uint4 digits[KR_WAVES][WORDS / 4][64];    // each lane's written and read by itself
+};
+
+template <int DT>
+__device__ __forceinline__ KaWords kr_fetch_keys(const unsigned char* head, int U, int piece) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int slot = DT == 64 ? 32 * piece + 16 * (g >> 1) + n : 16 * piece + n, u = min(DT == 64 ? g & 1 : g, U - 1);
+  return *reinterpret_cast<const KaWords*>(head + (u32)(slot * U + u) * 12);
+}
+// keys of page `pk`, values of page `pv`, scales of page `pk`
+template <int DT>
+__device__ __forceinline__ void kr_fetch(const unsigned char* pk, const unsigned char* pv, int U, int wave, KrRaw& raw) {
+  if (DT == 128 || wave >= 4) raw.k = kr_fetch_keys<DT>(pk, U, DT == 64 ? wave - 4 : wave);
+  if (DT == 128 || wave < 4) raw.v = ka_load_values<DT>(pv, U, wave);
+  if (wave < 4) raw.s = reinterpret_cast<const float*>(pk + kp_scale_off(U))[threadIdx.x];      // waves 0, 1: keys'; 2, 3: values'
+}
+template <int DT>
+__device__ __forceinline__ void kr_widen_keys(const KaWords& w, int piece, KrBundle<DT>& to) {
+  u32 o[4];
+  kp_expand(w.a, w.b, w.c, o);
+  to.keys[piece * 64 + (threadIdx.x & 63)] = make_uint4(o[0], o[1], o[2], o[3]);
+}
+// 32 tokens of a channel: nibble word v is tokens 8 v .. of the 32, the operand of lane group 2 (g % 2) + v / 2, tokens' quarter
+// 2 (g / 2) + v % 2.
+template <int DT>
+__device__ __forceinline__ void kr_widen_values(u32 o, int v, int d, KrBundle<DT>& to) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const u32 x[4] = {__builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(o, 1.0f, 0)),
+                    __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(o, 1.0f, 1)),
+                    __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(o, 1.0f, 2)),
+                    __builtin_bit_cast(u32, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(o, 1.0f, 3))};
+  to.vals[(d * 4 + 2 * (g >> 1) + (v & 1)) * 64 + 16 * (2 * (g & 1) + (v >> 1)) + n] = make_uint4(x[0], x[1], x[2], x[3]);
+}
+// the sequence's first token, in place of its entry there: level / 2 = mag + low / 2, of the sign in C
+template <int DT>
+__device__ __forceinline__ void kr_first_value(const KaWords& w, int d, const u32* lows, int U, KrBundle<DT>& to) {
+  const int lane = threadIdx.x & 63, c0 = min(16 * d, 32 * U - 16);
+  const u32 low = (lows[U + (c0 >> 5)] >> kp_sign_bit((c0 & 16) + (lane & 15))) & 1u;
+  const float m = (float)(w.a & 3u) + 0.5f * (float)low;
+  if (lane < 16) reinterpret_cast<uint16_t*>(to.vals + d * 256 + lane)[0] = (uint16_t)(__float_as_uint(w.c & 8u ? -m : m) >> 16);
+}
+// a page's scales as its rows take them: no value weight where no row of the workgroup sees the place, whatever stands there
+__device__ __forceinline__ void kr_scale(const KaArgs& p, const KaRange& all, int page, int wave, float s, KrScales& to) {
+  if (wave < 2) {
+    to.k[threadIdx.x] = page == 0 && threadIdx.x == 0 ? 2.0f * s : s;
+  } else {
+    const int tok = (int)threadIdx.x - KP_TOKENS;
+    to.v[tok] = KaSeen(p, (int64_t)page * KP_TOKENS, all.min_pos, all.max_pos, 0).at(tok) ? s : 0.0f;
+  }
+}
+
+// Scores of 16 tokens (QT x PARTS products) from their keys
+template <int DT, int QT, bool Q4, bool QV>
+__device__ __forceinline__ void kr_scores(uint4 key, const u32* dg, int t, v4f (&S)[QT][8]) {
+  typedef KaQuery<DT, Q4, QV> Query;
+  const int g = (threadIdx.x & 63) >> 4;
+  const u32 a[4] = {key.x, key.y, key.z, key.w};
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    S[i][t] = (v4f){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int d = 0; d < Query::PARTS; ++d) {
+      const u32* w = dg + (i * Query::PARTS + d) * 6;
+      S[i][t] = ka_mfma_qk(a, (v8i){(int)w[0], (int)w[1], (int)w[2], (int)w[3], (int)w[4], (int)w[5], 0, 0}, S[i][t], 127,
+                           Query::scale(d, g));
+    }
+  }
+}
+template <int DT>
+__device__ __forceinline__ uint4 kr_key(const KrBundle<DT>& bd, int t) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  return DT == 64 ? bd.keys[32 * t + 16 * (g & 1) + n] : bd.keys[t * 64 + lane];
+}
+template <int N>
+__device__ __forceinline__ void kr_digits(const uint4 (*digits)[64], u32 (&dg)[N]) {
+#pragma unroll
+  for (int j = 0; j < N / 4; ++j) {
+    const uint4 w = digits[j][threadIdx.x & 63];
+    dg[4 * j] = w.x; dg[4 * j + 1] = w.y; dg[4 * j + 2] = w.z; dg[4 * j + 3] = w.w;
+  }
+}
+// N times: one matrix instruction, then V of the vector unit's
+template <int N, int V>
+__device__ __forceinline__ void kr_interleave() {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x402, V, 0);
+  }
+}
+
+template <int DT, int QT, bool Q4, bool QV>
+__global__ __launch_bounds__(KR_THREADS) void kv_attention_rows_kernel(KaArgs p, int shift, int n_tiles) {
+  typedef KaQuery<DT, Q4, QV> Query;
+  typedef KrShared<DT, QT, Q4, QV> Shared;
+  extern __shared__ __align__(16) unsigned char ka_smem[];
+  Shared& sh = *reinterpret_cast<Shared*>(ka_smem);
+  const int h = (int)(blockIdx.x % (unsigned)p.H);
+  // late rows have the most pages: they go first
+  const int64_t item = n_tiles - 1 - (int64_t)(blockIdx.x / (unsigned)p.H);
+  KvSeq q;
+  const int64_t local = kp_find(p.b, item, p.G, shift, 1, q);
+  if (local < 0) return;                   // (whole workgroup)
+  const int rows = q.n * p.G;              // (at most T * G, which the host bounds)
+  if ((local << shift) >= rows) return;
+  const int block0 = (int)(local << shift), lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r0 = block0 + wave * (16 * QT);      // (a wave without rows has zero queries and does its share)
+  const int U = kp_units(p.D), hb = kp_head_bytes(U);
+  const KaRange all = ka_range(p, q, block0, KR_WAVES * 16 * QT, rows), rg = ka_range(p, q, r0 < rows ? r0 : block0, 16 * QT, rows);
+  uint4 (*digits)[64] = sh.digits[wave];
+  float qc[QT];
+  int qp[QT];
+  KaState<DT> st[QT];
+  {
+    u32 w[Shared::WORDS];
+    w[Shared::WORDS - 2] = w[Shared::WORDS - 1] = 0;
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      Query qy;
+      qy.load(p, q, r0 + 16 * i + n, rows, h);
+      qc[i] = qy.c;
+      qp[i] = qy.pos;
+#pragma unroll
+      for (int e = 0; e < Query::WORDS; ++e) w[i * Query::WORDS + e] = (u32)qy.op[0][e / 6][e % 6];
+      st[i].clear();
+    }
+#pragma unroll
+    for (int j = 0; j < Shared::WORDS / 4; ++j) digits[j][lane] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+  }
+
+  // the next four pages, nullptr behind the last
+  int k = -1;
+  int page[4] = {0, 0, 0, 0};
+  const unsigned char* head[4];
+  auto next = [&](int e) __attribute__((always_inline)) {
+    ++k;
+    head[e] = ka_next(p, q, all, h, hb, 1, k, page[e]);
+  };
+#pragma unroll
+  for (int e = 0; e < 4; ++e) next(e);
+  if (head[0]) {
+    constexpr int MV = DT / 16 * QT / 2, MQ = QT * Query::PARTS;       // products beside a tile of scores: of values, of keys
+    v4f S[QT][8];
+    v4i P[QT][4];                          // bfloat16, column operands of 32 tokens each
+    u32 dg[Shared::WORDS];
+    KrRaw raw;
+    const bool has_k = DT == 128 || wave >= 4, has_v = DT == 128 || wave < 4;
+    const int kp = DT == 64 ? wave - 4 : wave;
+    auto values = [&](int v, const u32 (&o)[4], KrBundle<DT>& to) __attribute__((always_inline)) {
+      if (has_v) kr_widen_values<DT>(o[v], v, wave, to);
+    };
+    // bundle 0: the first page's values, which meet zeros, and the second's keys; the first's keys for now in the other buffer
+    kr_fetch<DT>(head[0], head[0], U, wave, raw);
+    {
+      u32 o[4];
+      if (has_k) kr_widen_keys<DT>(raw.k, kp, sh.bundle[1]);
+      kp_expand(raw.v.a, raw.v.b, raw.v.c, o);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) values(v, o, sh.bundle[0]);
+      if (wave < 4) kr_scale(p, all, page[0], wave, raw.s, sh.scales[0]);
+    }
+    kr_fetch<DT>(head[1] ? head[1] : head[0], head[0], U, wave, raw);
+    if (has_k) kr_widen_keys<DT>(raw.k, kp, sh.bundle[0]);
+    if (wave < 4) kr_scale(p, all, page[1], wave, raw.s, sh.scales[1]);
+    kr_fetch<DT>(head[2] ? head[2] : head[0], head[0], U, wave, raw);
+    __syncthreads();
+    kr_digits(digits, dg);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      kr_scores<DT, QT, Q4, QV>(kr_key(sh.bundle[1], t), dg, t, S);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (page[0] == 0) {                    // the first token's lowest bits (its scale is doubled in LDS)
+      const int u = min(DT == 64 ? g & 1 : g, U - 1);
+      const u32* lows = reinterpret_cast<const u32*>(head[0] + kp_low_off(U));
+      u32 a[4];
+      ka_low_keys(n == 0 ? lows[u] : 0u, n == 0 ? reinterpret_cast<const u32*>(head[0])[u * 3 + 2] : 0u, a);
+#pragma unroll
+      for (int i = 0; i < QT; ++i)
+#pragma unroll
+        for (int d = 0; d < Query::PARTS; ++d) {
+          const u32* w = dg + (i * Query::PARTS + d) * 6;
+          S[i][0] = ka_mfma_qk(a, (v8i){(int)w[0], (int)w[1], (int)w[2], (int)w[3], (int)w[4], (int)w[5], 0, 0}, S[i][0], 126,
+                               Query::scale(d, g));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < QT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) P[i][e] = (v4i){0, 0, 0, 0};
+    __syncthreads();
+
+    for (int turn = 0; head[0]; ++turn) {
+      const KrScales& sc = sh.scales[turn & 3];
+      const KrBundle<DT>& bd = sh.bundle[turn & 1];
+      KrBundle<DT>& to = sh.bundle[(turn & 1) ^ 1];
+      const float* sk = sc.k + 16 * g;
+      const float* sv = sc.v + 16 * g;
+      float mx[QT], base[QT];
+      {
+        // last page's products, this page's scales and maximum, this wave's share of the next bundle
+        constexpr int VP = DT / 32;        // operands of the values beside a tile of scores
+        uint4 va[VP];
+        float4 s4 = *reinterpret_cast<const float4*>(sk + ka_token(0, 0));
+        u32 o[4];
+#pragma unroll
+        for (int e = 0; e < VP; ++e) va[e] = bd.vals[e * 64 + lane];
+#pragma unroll
+        for (int i = 0; i < QT; ++i) mx[i] = -INFINITY;
+        KaWords first = raw.v;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          uint4 vb[VP];
+          const float4 s = s4;
+#pragma unroll
+          for (int e = 0; e < VP; ++e) {
+            vb[e] = va[e];
+            if (t < 7) va[e] = bd.vals[((t + 1) * VP + e) * 64 + lane];
+          }
+          if (t < 7) s4 = *reinterpret_cast<const float4*>(sk + ka_token(t + 1, 0));
+#pragma unroll
+          for (int e = 0; e < VP; ++e) {
+            const int at = t * VP + e;
+#pragma unroll
+            for (int i = 0; i < QT; ++i)
+              st[i].o[at / 4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, vb[e]), __builtin_bit_cast(v8bf, P[i][at % 4]),
+                                                                        st[i].o[at / 4], 0, 0, 0);
+          }
+#pragma unroll
+          for (int i = 0; i < QT; ++i) {
+            S[i][t][0] *= s.x; S[i][t][1] *= s.y; S[i][t][2] *= s.z; S[i][t][3] *= s.w;
+            mx[i] = ka_max3(ka_max3(mx[i], S[i][t][0], S[i][t][1]), S[i][t][2], S[i][t][3]);
+          }
+          if (t == 0 && has_k) kr_widen_keys<DT>(raw.k, kp, to);
+          if (t == 1) kp_expand(raw.v.a, raw.v.b, raw.v.c, o);
+          if (t >= 2 && t < 6) values(t - 2, o, to);
+          kr_interleave<MV, 24 / MV>();
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        // (products done here, not where they are used)
+#pragma unroll
+        for (int i = 0; i < QT; ++i)
+#pragma unroll
+          for (int d = 0; d < DT / 16; ++d) asm volatile("" : "+v"(st[i].o[d]));
+        if (wave < 4) kr_scale(p, all, page[2], wave, raw.s, sh.scales[(turn + 2) & 3]);
+        if (page[0] == 0 && has_v) kr_first_value<DT>(first, wave, reinterpret_cast<const u32*>(head[0] + kp_low_off(U)), U, to);
+      }
+      kr_fetch<DT>(head[3] ? head[3] : head[0], head[1] ? head[1] : head[0], U, wave, raw);
+      const int64_t t0 = (int64_t)page[0] * KP_TOKENS;
+      if (ka_masked(p, rg, t0)) {
+#pragma unroll
+        for (int i = 0; i < QT; ++i) {
+          ka_mask<1>(S[i], KaSeen(p, t0, qp[i], qp[i], 16 * g));
+          mx[i] = -INFINITY;
+#pragma unroll
+          for (int t = 0; t < 8; ++t) mx[i] = ka_max3(ka_max3(mx[i], S[i][t][0], S[i][t][1]), S[i][t][2], S[i][t][3]);
+        }
+      }
+      ka_raise<DT, 16, QT>(mx, qc, st, base);
+      __builtin_amdgcn_sched_barrier(0);
+      {
+        float sum[QT][2];
+        uint4 key = kr_key(bd, 0);
+        float4 s4 = *reinterpret_cast<const float4*>(sv + ka_token(0, 0));
+        kr_digits(digits, dg);
+#pragma unroll
+        for (int i = 0; i < QT; ++i) sum[i][0] = sum[i][1] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          const float vs[4] = {s4.x, s4.y, s4.z, s4.w};
+          if (t < 7) s4 = *reinterpret_cast<const float4*>(sv + ka_token(t + 1, 0));
+          if (t > 0) {
+            const uint4 now = key;
+            key = kr_key(bd, t);
+            kr_scores<DT, QT, Q4, QV>(now, dg, t - 1, S);
+          }
+#pragma unroll
+          for (int i = 0; i < QT; ++i) {
+            float w[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(S[i][t][r], qc[i], -base[i]));
+              sum[i][r & 1] += e;
+              w[r] = ka_mul_legacy(e, vs[r]);
+            }
+            P[i][t >> 1][2 * (t & 1)] = __builtin_bit_cast(int, (v2bf){(__bf16)w[0], (__bf16)w[1]});
+            P[i][t >> 1][2 * (t & 1) + 1] = __builtin_bit_cast(int, (v2bf){(__bf16)w[2], (__bf16)w[3]});
+          }
+          if (t > 0) kr_interleave<MQ, QT * 18 / MQ>();
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        kr_scores<DT, QT, Q4, QV>(key, dg, 7, S);          // (behind the last page: of nothing, for nobody)
+#pragma unroll
+        for (int i = 0; i < QT; ++i) {
+          st[i].l += sum[i][0] + sum[i][1];
+          asm volatile("" : "+v"(P[i][0]), "+v"(P[i][1]), "+v"(P[i][2]), "+v"(P[i][3]), "+v"(st[i].l));
+#pragma unroll
+          for (int t = 0; t < 8; ++t) asm volatile("" : "+v"(S[i][t]));
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 3; ++e) { head[e] = head[e + 1]; page[e] = page[e + 1]; }
+      next(3);
+      if (!head[0]) {                      // the last page's products
+        const KrBundle<DT>& last = sh.bundle[(turn & 1) ^ 1];
+#pragma unroll
+        for (int at = 0; at < DT / 4; ++at)
+#pragma unroll
+          for (int i = 0; i < QT; ++i)
+            st[i].o[at / 4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, last.vals[at * 64 + lane]),
+                                                                      __builtin_bit_cast(v8bf, P[i][at % 4]), st[i].o[at / 4], 0, 0, 0);
+      }
+    }
+  }
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
     float l = st[i].l;
@@ -980,6 +1353,14 @@ static KaPlan ka_plan(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t m
   return {(int)(want < most ? want : most), shift};
 }
 
+// Whole rows, up to 128 channels: eight waves of 32 rows (8), or of 16 (7) where 32 give less than a workgroup to every CU (4 sequences
+// of 256 on 2000 cached, 8 heads of 128: 59 us with 16, 88 with 32) or about one and the rows see very unlike numbers of pages, being
+// most of their sequences (4096 on none, 16 heads: 109 and 144; 2048 on 6144, 8 heads, the other way about: 281 and 254).
+static int ka_rows_shift(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t max_pages) {
+  const int64_t blocks = ka_tiles(T, G, n_seqs, 8) * H;
+  return blocks >= 512 || (blocks >= 256 && 2 * T <= n_seqs * max_pages * KP_TOKENS) ? 8 : 7;
+}
+
 size_t bl_kv_attention_ws_bytes(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t D, int64_t max_pages) {
   const KaPlan k = ka_plan(T, n_seqs, G, H, max_pages);
   if (k.splits <= 1) return 0;
@@ -1008,11 +1389,18 @@ int bl_launch_kv_attention(const void* Q, int64_t ldq, bl_dtype qdt, int Hq, int
     if (p.splits && shift == 2) kv_attention_split_kernel<DT, 4, Q4, QV><<<blocks, KA_THREADS, 0, s>>>(p); \
     else if (p.splits && shift == 3) kv_attention_split_kernel<DT, 8, Q4, QV><<<blocks, KA_THREADS, 0, s>>>(p); \
     else if (p.splits) kv_attention_split_kernel<DT, 16, Q4, QV><<<blocks, KA_THREADS, 0, s>>>(p);       \
-    else {                                                                                               \
-      constexpr int lds = (int)(2 * sizeof(KaStage<DT>)) + KA_WAVES * 64 * 4 * KA_QT(DT) * KaQuery<DT, Q4, QV>::WORDS; \
-      BL_SET_MAX_LDS_ONCE((kv_attention_rows_kernel<DT, KA_QT(DT), Q4, QV>), lds);                       \
-      kv_attention_rows_kernel<DT, KA_QT(DT), Q4, QV><<<blocks, KA_THREADS, lds, s>>>(p, shift, (int)tiles); \
-    }                                                                                                    \
+    else if (DT == 256) {                                                                                \
+      constexpr int lds = (int)(2 * sizeof(KaStage<256>)) + KA_WAVES * 64 * 4 * KaQuery<256, Q4, QV>::WORDS; \
+      BL_SET_MAX_LDS_ONCE((kv_attention_wide_kernel<256, 1, Q4, QV>), lds);                              \
+      kv_attention_wide_kernel<256, 1, Q4, QV><<<blocks, KA_THREADS, lds, s>>>(p, shift, (int)tiles);    \
+    } else if (shift == 8) KA_ROWS((DT == 64 ? 64 : 128), 2, Q4, QV);                                    \
+    else KA_ROWS((DT == 64 ? 64 : 128), 1, Q4, QV);                                                      \
+  } while (0)
+#define KA_ROWS(DT, QT, Q4, QV)                                                                          \
+  do {                                                                                                   \
+    constexpr int lds = (int)sizeof(KrShared<DT, QT, Q4, QV>);                                           \
+    BL_SET_MAX_LDS_ONCE((kv_attention_rows_kernel<DT, QT, Q4, QV>), lds);                                \
+    kv_attention_rows_kernel<DT, QT, Q4, QV><<<blocks, KR_THREADS, lds, s>>>(p, shift, (int)tiles);      \
   } while (0)
 #define KA_GO(DT)                                                  \
   do {                                                             \
@@ -1022,7 +1410,7 @@ int bl_launch_kv_attention(const void* Q, int64_t ldq, bl_dtype qdt, int Hq, int
       if (qv) KA_GO2(DT, false, true); else KA_GO2(DT, false, false); \
     }                                                              \
   } while (0)
-  const int shift = p.splits ? plan.shift : 6 + (KA_QT(dt) == 2);           // four waves of KA_QT tiles of 16 rows
+  const int shift = p.splits ? plan.shift : dt == 256 ? 6 : ka_rows_shift(b.T, b.n_seqs, p.G, H, b.max_pages);
   const int64_t tiles = ka_tiles(b.T, p.G, b.n_seqs, shift);
   const int64_t n_blocks = tiles * H * (p.splits ? p.splits : 1);
   p.slots = tiles % b.n_seqs == 0 ? (int)(tiles / b.n_seqs) : 1;
@@ -1039,5 +1427,6 @@ int bl_launch_kv_attention(const void* Q, int64_t ldq, bl_dtype qdt, int Hq, int
   }
 #undef KA_GO
 #undef KA_GO2
+#undef KA_ROWS
   return BL_OK;
 }
