@@ -447,6 +447,15 @@ def _batch(pages, page_table, q_start, kv_len, rope, H, D, T):
     return pages.shape[0], n_seqs, page_table.shape[1], 0 if rope is None else rope.shape[0]
 
 
+def _scratch(ws, n, device):
+    """A call's workspace of n bytes: the caller's, which has to be on the tensors' device, or a new one (None: none needed)."""
+    if ws is None:
+        return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+    if _dev(ws).device != device:
+        raise ValueError("workspace on %s expected" % device)
+    return ws
+
+
 def kv_pages_new(n_pages, H, D, device):
     """A pool of empty pages (128 positions each, keys and values of H heads of D channels)."""
     n = lib().kv_page_bytes(H, D)
@@ -494,8 +503,7 @@ def kv_pages_attention(Q, pages, page_table, q_start, kv_len, H, rope=None, scal
     n_pages, n_seqs, max_pages, n_pos = _batch(pages, page_table, q_start, kv_len, rope, H, D, T)
     L = lib()
     n = L.kv_pages_attention_workspace_bytes(T, n_seqs, Hq, H, D, max_pages)
-    if ws is None and n:
-        ws = torch.empty(n, dtype=torch.uint8, device=Q.device)
+    ws = _scratch(ws, n, Q.device)
     O = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=Q.device) if out is None else out
     if _dev(O).dtype != torch.bfloat16 or O.shape != Q.shape or O.device != Q.device:
         raise ValueError("bfloat16 output [T, Hq, D] expected")
@@ -547,9 +555,7 @@ def rmsnorm_backward(dY, H, rstd, gamma, dH=None, ws=None):
     _per(gamma, K, H.device)
     _per(rstd, M, H.device)
     L = lib()
-    n = L.rmsnorm_backward_workspace_bytes(M, K)
-    if ws is None:
-        ws = torch.empty(n, dtype=torch.uint8, device=H.device)
+    ws = _scratch(ws, L.rmsnorm_backward_workspace_bytes(M, K), H.device)
     dX = torch.empty_like(H)
     dgamma = torch.empty(K, dtype=torch.float32, device=H.device)
     with _on(H):

@@ -140,3 +140,14 @@ def test_two_streams_with_their_own_workspaces():
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+def test_workspace_of_another_device_is_refused():
+    h, rstd, gamma = (torch.ones(s, device="cuda") for s in ((3, 64), (3,), (64,)))
+    ws = torch.zeros(1 << 20, dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        B.rmsnorm_backward(h, h, rstd, gamma, ws=ws)
+    pages, table = B.kv_pages_new(1, 1, 64, "cuda"), i32(0).view(1, 1)
+    q = torch.zeros((1, 1, 64), dtype=BF16, device="cuda")
+    with pytest.raises(ValueError):
+        B.kv_pages_attention(q, pages, table, i32(0, 1), i32(1), 1, ws=ws)

@@ -83,3 +83,26 @@ def test_masked_places_may_hold_anything(new, ctx, H, Hq, pages, D):
     good = B.kv_pages_attention(Q, pages_d, table, qs, ln, H).float().cpu().numpy()
     rows = new[0] - 40
     assert np.array_equal(bad[:rows], good[:rows]) and np.isfinite(clean[:b.q_start[-1]]).all()
+
+
+@pytest.mark.parametrize("new,ctx,H,Hq,pages,D", [SETS[1], SETS[5], SETS[3]])
+def test_captured_and_replayed(new, ctx, H, Hq, pages, D):
+    """The graph takes the queries and lengths that stand there at each replay."""
+    b = batch(new, ctx, H, Hq, pages, D, 36)
+    pages_d, table, qs, ln = b.dev()
+    g = torch.Generator().manual_seed(5)
+    Q = torch.randn(b.T, Hq, D, generator=g).to(torch.bfloat16).cuda()
+    out = torch.zeros(b.T, Hq, D, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.kv_pages_attention(Q, pages_d, table, qs, ln, H, window=200, sinks=1, out=out)
+    full = ln.clone()
+    for k in range(4):
+        Q.copy_(torch.randn(b.T, Hq, D, generator=g))
+        ln.copy_(full - 30 * k)
+        graph.replay()
+        want = B.kv_pages_attention(Q, pages_d, table, qs, ln, H, window=200, sinks=1)
+        torch.cuda.synchronize()
+        rows = int(b.q_start[-1])
+        assert torch.equal(out[:rows], want[:rows]), k
