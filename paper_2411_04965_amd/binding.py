@@ -121,6 +121,9 @@ def _native():
             loader.exec_module(m)
             m.use(*(ctypes.cast(f, _vp).value for f in (L.bitlinear_a4, L.bitlinear_a8_sparse, L.bitlinear_a4_gate_up,
                                                         L.bitlinear_workspace_bytes, L.bitlinear_gate_up_workspace_bytes)))
+            m.use_attention(*(ctypes.cast(f, _vp).value for f in (
+                L.rmsnorm_quantize, L.quantize_act_bytes, L.kv_pages_append, L.kv_pages_attention,
+                L.kv_pages_attention_workspace_bytes, L.kv_page_bytes)))
             _marshal = m
         except ImportError as e:
             _marshal = False
@@ -467,6 +470,11 @@ def kv_pages_new(n_pages, H, D, device):
 def kv_pages_append(K, V, pages, page_table, q_start, kv_len, rope=None, eps=DEFAULT_EPS):
     """Quantizes K (rotated where `rope` is given) and V [T, H, D] into their pages: rows q_start[s] .. q_start[s + 1] - 1 are the
     last positions of sequence s, whose length with them is kv_len[s].  Rows may be a stride apart."""
+    m = _marshal or _native()
+    if m:
+        r = m.kv_append(K, V, pages, page_table, q_start, kv_len, rope, eps)
+        if r is not None:
+            return _check("kv_pages_append", r)
     ldk, ldv = _rows(K), _rows(V)
     if K.shape != V.shape or K.dtype != V.dtype or K.device != pages.device or V.device != pages.device:
         raise ValueError("K and V of one shape, type and device expected")
@@ -496,6 +504,11 @@ def kv_pages_attention(Q, pages, page_table, q_start, kv_len, H, rope=None, scal
                        eps=DEFAULT_EPS, ws=None, out=None):
     """Causal attention of the batch's rows Q [T, Hq, D] over the cache's H heads -> O bfloat16 [T, Hq, D].  scale: D^-0.5 if None;
     window > 0: a row sees its last `window` positions and the sequence's first `sinks`."""
+    m = _marshal or _native()
+    if m:
+        r = m.kv_attention(Q, pages, page_table, q_start, kv_len, H, rope, scale, window, sinks, q_bits, eps, ws, out)
+        if r is not None:
+            return _done("kv_pages_attention", r)
     ldq = _rows(Q)
     T, Hq, D = Q.shape
     if Q.device != pages.device:
@@ -530,6 +543,11 @@ def _per(t, n, device):
 def rmsnorm_quantize(X, gamma, mode, residual=None, norm_eps=1e-5, eps=DEFAULT_EPS):
     """h = X (+ residual), RMS norm with weights gamma, codes of the result in `mode` -> dict(q, scale, h, rstd); q and scale as
     quantize_act's (BL_ACT_TOPK_INT8_ABSMAX keeps every channel); h is X itself where there is no residual."""
+    m = _marshal or _native()
+    if m:
+        r = m.norm(X, gamma, mode, residual, norm_eps, eps)
+        if r is not None:
+            return _done("rmsnorm_quantize", r)
     _dev(X)
     M, K = X.shape
     _same(X, residual)

@@ -1,4 +1,4 @@
-// Argument marshalling of the linears a serving loop calls most, as a Python module.  The same calls through ctypes cost 2.4 us
+// Argument marshalling of the linears, the norm, the cache and the attention a serving loop calls most, as a Python module.  The same calls through ctypes cost 2.4 us
 // of host time each beside the launches (3.5 us more where workspace and output are allocated), and small layers are bound
 // by the host.  Here plain tensors are unpacked directly: 0.7 us, and 1.5 us for both allocations.
 //
@@ -15,6 +15,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <exception>
 
 #include "../../include/bitlinear.h"
@@ -29,10 +30,19 @@ struct {
   decltype(&::bitlinear_workspace_bytes) workspace_bytes;
   decltype(&::bitlinear_gate_up_workspace_bytes) gate_up_workspace_bytes;
 } lib;
+struct {
+  decltype(&::rmsnorm_quantize) norm;
+  decltype(&::quantize_act_bytes) act_bytes;
+  decltype(&::kv_pages_append) append;
+  decltype(&::kv_pages_attention) attention;
+  decltype(&::kv_pages_attention_workspace_bytes) attention_bytes;
+  decltype(&::kv_page_bytes) page_bytes;
+} att;
 
 PyObject* get_device = nullptr;    // torch._C._cuda_getDevice
 PyObject* get_stream = nullptr;    // torch._C._cuda_getCurrentRawStream
 PyObject* str_H = nullptr;
+PyObject *str_q = nullptr, *str_scale = nullptr, *str_h = nullptr, *str_rstd = nullptr;
 
 struct NotPlain {};
 
@@ -256,22 +266,206 @@ PyObject* gate_up(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (addresses of bitlinear_a4, bitlinear_a8_sparse, bitlinear_a4_gate_up, bitlinear_workspace_bytes, bitlinear_gate_up_workspace_bytes)
-PyObject* use(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void* p[5];
-  if (n != 5) {
-    PyErr_SetString(PyExc_TypeError, "five addresses expected");
-    return nullptr;
+// A device's tensors: contiguous, of one type, on the device that is the current one (its stream is the call's)
+struct Place {
+  int index;
+  at::Device device;
+  explicit Place(const at::Tensor& t) : index(0), device(t.device()) {
+    if (!t.is_cuda()) throw NotPlain();
+    PyObject* const d = PyObject_CallNoArgs(get_device);
+    if (!d) throw std::exception_ptr();
+    index = (int)PyLong_AsLong(d);
+    Py_DECREF(d);
+    if (device.index() != index) throw NotPlain();
   }
-  for (int i = 0; i < 5; ++i) {
+  const at::Tensor& dense(PyObject* o, at::ScalarType type) const {
+    const at::Tensor& t = tensor(o);
+    if (t.device() != device || !t.is_contiguous() || t.scalar_type() != type) throw NotPlain();
+    return t;
+  }
+};
+
+// [T, heads, D] rows a stride apart, as the binding's _rows has them
+int64_t rows(const at::Tensor& x, const Place& at) {
+  if (x.device() != at.device || x.dim() != 3) throw NotPlain();
+  if ((x.size(2) > 1 && x.stride(2) != 1) || (x.size(1) > 1 && x.stride(1) != x.size(2))) throw NotPlain();
+  return x.size(0) > 1 ? x.stride(0) : x.size(1) * x.size(2);
+}
+
+// pages, page table, row starts, lengths and rotations, as the binding's _batch checks them
+struct Paged {
+  void *pages, *table, *q_start, *kv_len, *rope = nullptr;
+  int64_t n_pages, n_seqs, max_pages, n_pos = 0;
+  Paged(PyObject* p, PyObject* t, PyObject* qs, PyObject* ln, PyObject* r, int64_t H, int64_t D, const Place& at) {
+    const at::Tensor& pg = at.dense(p, at::kByte);
+    const at::Tensor& tb = at.dense(t, at::kInt);
+    const at::Tensor& q = at.dense(qs, at::kInt);
+    const at::Tensor& l = at.dense(ln, at::kInt);
+    n_seqs = l.numel();
+    if (tb.dim() != 2 || tb.size(0) != n_seqs || q.numel() != n_seqs + 1) throw NotPlain();
+    if (pg.dim() != 2 || pg.size(1) != (int64_t)att.page_bytes(H, D)) throw NotPlain();
+    if (r != Py_None) {
+      const at::Tensor& f = at.dense(r, at::kFloat);
+      if (f.dim() != 2 || f.size(1) != D) throw NotPlain();
+      rope = f.data_ptr();
+      n_pos = f.size(0);
+    }
+    pages = pg.data_ptr();
+    table = tb.data_ptr();
+    q_start = q.data_ptr();
+    kv_len = l.data_ptr();
+    n_pages = pg.size(0);
+    max_pages = tb.size(1);
+  }
+};
+
+// (K, V, pages, page_table, q_start, kv_len, rope, eps) -> 0
+PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 8, [&]() -> PyObject* {
+    const at::Tensor &k = tensor(a[0]), &v = tensor(a[1]);
+    const Place at(k);
+    const int64_t ldk = rows(k, at), ldv = rows(v, at);
+    if (k.sizes() != v.sizes() || k.scalar_type() != v.scalar_type()) throw NotPlain();
+    const int dt = dtype_code(k.scalar_type());
+    const int64_t T = k.size(0), H = k.size(1), D = k.size(2);
+    const Paged b(a[2], a[3], a[4], a[5], a[6], H, D, at);
+    const float eps = real(a[7]);
+    void *const kp = k.data_ptr(), *const vp = v.data_ptr(), *const s = stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = att.append(kp, ldk, vp, ldv, (bl_dtype)dt, T, H, D, (const int32_t*)b.q_start, (const int32_t*)b.kv_len, b.n_seqs,
+                    (const int32_t*)b.table, b.max_pages, (const float*)b.rope, b.n_pos, eps, b.pages, b.n_pages, s);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+  });
+}
+
+// (Q, pages, page_table, q_start, kv_len, H, rope, scale, window, sinks, q_bits, eps, ws, out)
+PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 14, [&]() -> PyObject* {
+    const at::Tensor& q = tensor(a[0]);
+    const Place at(q);
+    const int64_t ldq = rows(q, at), T = q.size(0), Hq = q.size(1), D = q.size(2), H = integer(a[5]);
+    const int dt = dtype_code(q.scalar_type());
+    const Paged b(a[1], a[2], a[3], a[4], a[6], H, D, at);
+    if (D < 1) throw NotPlain();
+    const float scale = a[7] == Py_None ? (float)std::pow((double)D, -0.5) : real(a[7]), eps = real(a[11]);
+    const int64_t window = integer(a[8]), sinks = integer(a[9]), q_bits = integer(a[10]);
+    if (q_bits != 16 && q_bits != 4) throw NotPlain();
+    const auto options = q.options().requires_grad(false);
+    at::Tensor ws, own;
+    size_t bytes = att.attention_bytes(T, b.n_seqs, Hq, H, D, b.max_pages);
+    void* wp = nullptr;
+    if (a[12] != Py_None) {
+      const at::Tensor& t = tensor(a[12]);
+      if (t.device() != at.device || !t.is_contiguous()) throw NotPlain();
+      wp = t.data_ptr();
+      bytes = t.nbytes();
+    } else if (bytes) {
+      ws = at::empty({(int64_t)bytes}, options.dtype(at::kByte));
+      wp = ws.data_ptr();
+    }
+    void* op;
+    if (a[13] != Py_None) {
+      const at::Tensor& t = at.dense(a[13], at::kBFloat16);
+      if (t.sizes() != q.sizes()) throw NotPlain();
+      op = t.data_ptr();
+    } else {
+      own = at::empty({T, Hq, D}, options.dtype(at::kBFloat16));
+      op = own.data_ptr();
+    }
+    void *const qp = q.data_ptr(), *const s = stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = att.attention(qp, ldq, (bl_dtype)dt, T, Hq, H, D, (int)q_bits, (const int32_t*)b.q_start, (const int32_t*)b.kv_len, b.n_seqs,
+                       (const int32_t*)b.table, b.max_pages, (const float*)b.rope, b.n_pos, scale, eps, window, sinks, b.pages,
+                       b.n_pages, op, wp, bytes, s);
+    Py_END_ALLOW_THREADS
+    if (rc) return PyLong_FromLong(rc);
+    if (a[13] == Py_None) return THPVariable_Wrap(std::move(own));
+    Py_INCREF(a[13]);
+    return a[13];
+  });
+}
+
+// (X, gamma, mode, residual, norm_eps, eps) -> dict(q, scale, h, rstd)
+PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 6, [&]() -> PyObject* {
+    const Input in(a[0]);
+    const Place at(in.x);
+    const at::Tensor& g = at.dense(a[1], at::kFloat);
+    const int64_t mode = integer(a[2]);
+    if (in.M < 1 || in.K < 1 || g.numel() != in.K || mode < 0 || mode > 64) throw NotPlain();
+    const float norm_eps = real(a[4]), eps = real(a[5]);
+    const void* r = nullptr;
+    const auto options = in.x.options().requires_grad(false);
+    at::Tensor h;
+    void* hp = nullptr;
+    if (a[3] != Py_None) {
+      const at::Tensor& t = at.dense(a[3], in.x.scalar_type());
+      if (t.sizes() != in.x.sizes()) throw NotPlain();
+      r = t.data_ptr();
+      h = at::empty({in.M, in.K}, options);
+      hp = h.data_ptr();
+    }
+    const size_t bytes = att.act_bytes((bl_act_mode)mode, in.M, in.K);
+    if (!bytes) throw NotPlain();
+    at::Tensor q = at::empty({(int64_t)bytes}, options.dtype(at::kByte));
+    at::Tensor scale = at::empty({in.M}, options.dtype(at::kFloat)), rstd = at::empty({in.M}, options.dtype(at::kFloat));
+    void* const s = stream();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = att.norm(in.p, r, (bl_dtype)in.dt, in.M, in.K, (const float*)g.data_ptr(), norm_eps, (bl_act_mode)mode, eps, hp,
+                  (float*)rstd.data_ptr(), q.data_ptr(), (float*)scale.data_ptr(), s);
+    Py_END_ALLOW_THREADS
+    if (rc) return PyLong_FromLong(rc);
+    PyObject* const d = PyDict_New();
+    if (!d) return nullptr;
+    bool bad = false;
+    auto put = [&](PyObject* key, PyObject* v) {
+      bad = bad || !v || PyDict_SetItem(d, key, v) != 0;
+      Py_XDECREF(v);
+    };
+    put(str_q, THPVariable_Wrap(std::move(q)));
+    put(str_scale, THPVariable_Wrap(std::move(scale)));
+    if (hp) put(str_h, THPVariable_Wrap(std::move(h)));
+    else { Py_INCREF(a[0]); put(str_h, a[0]); }
+    put(str_rstd, THPVariable_Wrap(std::move(rstd)));
+    if (bad) { Py_DECREF(d); return nullptr; }
+    return d;
+  });
+}
+
+// (addresses of bitlinear_a4, bitlinear_a8_sparse, bitlinear_a4_gate_up, bitlinear_workspace_bytes, bitlinear_gate_up_workspace_bytes)
+template <size_t N>
+bool addresses(PyObject* const* a, Py_ssize_t n, void* (&p)[N]) {
+  if (n != (Py_ssize_t)N) {
+    PyErr_Format(PyExc_TypeError, "%zu addresses expected", N);
+    return false;
+  }
+  for (size_t i = 0; i < N; ++i) {
     p[i] = PyLong_AsVoidPtr(a[i]);
     if (!p[i]) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address");
-      return nullptr;
+      return false;
     }
   }
+  return true;
+}
+PyObject* use(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void* p[5];
+  if (!addresses(a, n, p)) return nullptr;
   lib = {(decltype(lib.a4))p[0], (decltype(lib.a8_sparse))p[1], (decltype(lib.gate_up))p[2], (decltype(lib.workspace_bytes))p[3],
          (decltype(lib.gate_up_workspace_bytes))p[4]};
+  Py_RETURN_NONE;
+}
+// (addresses of rmsnorm_quantize, quantize_act_bytes, kv_pages_append, kv_pages_attention, kv_pages_attention_workspace_bytes,
+// kv_page_bytes)
+PyObject* use_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void* p[6];
+  if (!addresses(a, n, p)) return nullptr;
+  att = {(decltype(att.norm))p[0], (decltype(att.act_bytes))p[1], (decltype(att.append))p[2], (decltype(att.attention))p[3],
+         (decltype(att.attention_bytes))p[4], (decltype(att.page_bytes))p[5]};
   Py_RETURN_NONE;
 }
 
@@ -280,6 +474,10 @@ PyMethodDef methods[] = {
     {"a4", (PyCFunction)(void (*)(void))a4, METH_FASTCALL, "bitlinear_a4"},
     {"a8_sparse", (PyCFunction)(void (*)(void))a8_sparse, METH_FASTCALL, "bitlinear_a8_sparse"},
     {"gate_up", (PyCFunction)(void (*)(void))gate_up, METH_FASTCALL, "bitlinear_a4_gate_up, H only"},
+    {"use_attention", (PyCFunction)(void (*)(void))use_attention, METH_FASTCALL, "those of the three below, by address"},
+    {"norm", (PyCFunction)(void (*)(void))norm, METH_FASTCALL, "rmsnorm_quantize"},
+    {"kv_append", (PyCFunction)(void (*)(void))kv_append, METH_FASTCALL, "kv_pages_append"},
+    {"kv_attention", (PyCFunction)(void (*)(void))kv_attention, METH_FASTCALL, "kv_pages_attention"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "bitlinear_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -298,5 +496,9 @@ PyMODINIT_FUNC PyInit_bitlinear_marshal() {
     return nullptr;
   }
   str_H = PyUnicode_InternFromString("H");
-  return str_H ? PyModule_Create(&module) : nullptr;
+  str_q = PyUnicode_InternFromString("q");
+  str_scale = PyUnicode_InternFromString("scale");
+  str_h = PyUnicode_InternFromString("h");
+  str_rstd = PyUnicode_InternFromString("rstd");
+  return str_H && str_q && str_scale && str_h && str_rstd ? PyModule_Create(&module) : nullptr;
 }

@@ -3,8 +3,8 @@
 // HBM bound: a bfloat16 channel takes 4 bytes in, 2 out, and half a byte (INT4) to one (INT8) of codes.  One workgroup has a row in
 // registers, 16 channels a thread and turn (a thread then owns whole words of every code format), so the row is read once though
 // it is passed over three times: squares, statistic, codes.  The two sums are float64 (as the quantizers' mean is), so that the
-// codes do not depend on the order of the additions.  16384 x 4096 with a residual, six-bit codes: 102 us = 4.3 TB/s; 2000 x 5460, INT8, rows
-// off the 16-byte boundaries: 24 us = 3.2 TB/s; one row of 4096: 3.6 us, launch and two exchanges between waves.
+// codes do not depend on the order of the additions.  16384 x 4096 with a residual, six-bit codes: 102 us = 4.3 TB/s; 2000 x 5460, INT8:
+// 24 us = 3.2 TB/s; one row of 4096: 3.6 us, launch and two exchanges between waves.
 #include "common.h"
 
 typedef u32 u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
