@@ -583,6 +583,13 @@ __device__ __forceinline__ void ka_store(const KaArgs& p, const KvSeq& q, int r,
   }
 }
 
+// Late rows have the most pages: they go first.  Where every sequence has as many items, all last ones go before all others: most are
+// empty, and in turn with full ones they would leave half of the CUs without work (below; 32 sequences of 128 rows: 149 us in turn).
+__device__ __forceinline__ int64_t ka_late_first(const KaArgs& p, unsigned at, int n_tiles) {
+  if (p.slots > 1) return (int64_t)(at % (unsigned)p.b.n_seqs) * p.slots + (p.slots - 1 - (int)(at / (unsigned)p.b.n_seqs));
+  return n_tiles - 1 - (int64_t)at;
+}
+
 // Many rows, more than 128 channels: a workgroup has 4 x QT x 16 rows (row = new token x query head of the group) of one key / value
 // head and walks their pages; each wave widens a quarter of a page's codes into LDS, where all four read them as operands, while the
 // page before is worked on.  (The kernel below it, for up to 128 channels, keeps the values in bfloat16, for which LDS has no room here.)
@@ -761,8 +768,7 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attention_wide_kernel(KaArgs
   KaStage<DT>* stage = reinterpret_cast<KaStage<DT>*>(ka_smem);
   typedef KaQuery<DT, Q4, QV> Query;
   const int h = (int)(blockIdx.x % (unsigned)p.H);
-  // late rows have the most pages: they go first
-  const int64_t item = n_tiles - 1 - (int64_t)(blockIdx.x / (unsigned)p.H);
+  const int64_t item = ka_late_first(p, blockIdx.x / (unsigned)p.H, n_tiles);
   KvSeq q;
   const int64_t local = kp_find(p.b, item, p.G, shift, 1, q);
   if (local < 0) return;                   // (whole workgroup)
@@ -959,8 +965,7 @@ __global__ __launch_bounds__(KR_THREADS) void kv_attention_rows_kernel(KaArgs p,
   extern __shared__ __align__(16) unsigned char ka_smem[];
   Shared& sh = *reinterpret_cast<Shared*>(ka_smem);
   const int h = (int)(blockIdx.x % (unsigned)p.H);
-  // late rows have the most pages: they go first
-  const int64_t item = n_tiles - 1 - (int64_t)(blockIdx.x / (unsigned)p.H);
+  const int64_t item = ka_late_first(p, blockIdx.x / (unsigned)p.H, n_tiles);
   KvSeq q;
   const int64_t local = kp_find(p.b, item, p.G, shift, 1, q);
   if (local < 0) return;                   // (whole workgroup)
@@ -1341,11 +1346,15 @@ static int ka_dt(int64_t D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 struct KaPlan {
   int splits, shift;
 };
-static KaPlan ka_plan(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t max_pages) {
-  // Whole rows where there are enough of them for the workgroups of 128 (or 64) rows to be filled and to fill the chip: 1000 rows x 32
-  // heads of 64 channels without a cache 37 us, 56 split; 64 sequences x 16 rows x 8 heads, 2000 cached: 95 and 37; a chunk of 500 among
-  // 15 single tokens x 32 heads: 75 and 55.
-  if (T * G >= 64 * n_seqs && ka_tiles(T, G, n_seqs, 4) * H >= 512) return {0, 0};
+static KaPlan ka_plan(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t D, int64_t max_pages) {
+  // Whole rows where their workgroups (of 128, or 64, rows) are filled and fill the chip's turns: sequences taken to be alike, the share of
+  // the row places of all turns that have a row.  A place of the whole rows does about 1.6 times the work of one of the split ones (128
+  // channels; of more, 2.5).  Split / whole, 8 heads of 128: 1 sequence of 256 x 4 rows on 2000 cached (0.25 of the places) 30 / 54 us,
+  // of 400 x 4 on 4000 (0.39) 75 / 92, of 512 x 4 (0.5) 77 / 95; 8 of 200 on 900, 16 heads of 64 (0.78) 58 / 37; 1000 on none, 32 heads
+  // of 64 (0.98) 55 / 32; 16 heads of 256, 2 of 300 on 1000 (0.59) 76 / 54.
+  const int unit = D > 128 ? 64 : 128;
+  const int64_t rows = (T * G + n_seqs - 1) / n_seqs, blocks = (rows + unit - 1) / unit * n_seqs * H, turns = (blocks + 255) / 256;
+  if ((double)T * G * H >= (D > 128 ? 0.4 : 0.6) * 256.0 * turns * unit) return {0, 0};
   // rows a sequence: tiles of 4 or 8 do without the softmax of empty columns
   const int shift = T * G <= 4 * n_seqs ? 2 : T * G <= 8 * n_seqs ? 3 : 4;
   const int64_t tiles = ka_tiles(T, G, n_seqs, shift) * H;
@@ -1362,7 +1371,7 @@ static int ka_rows_shift(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_
 }
 
 size_t bl_kv_attention_ws_bytes(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t D, int64_t max_pages) {
-  const KaPlan k = ka_plan(T, n_seqs, G, H, max_pages);
+  const KaPlan k = ka_plan(T, n_seqs, G, H, D, max_pages);
   if (k.splits <= 1) return 0;
   return (size_t)(ka_tiles(T, G, n_seqs, k.shift) * H * k.splits * ka_part_floats(ka_dt(D), 1 << k.shift) * 4);
 }
@@ -1380,7 +1389,7 @@ int bl_launch_kv_attention(const void* Q, int64_t ldq, bl_dtype qdt, int Hq, int
   p.sinks = (int)(sinks < 0x7FFFFF00 ? sinks : 0x7FFFFF00);
   p.pages = (const unsigned char*)pages;
   p.O = (uint16_t*)O; p.part = (float*)ws;
-  const KaPlan plan = ka_plan(b.T, b.n_seqs, p.G, H, b.max_pages);
+  const KaPlan plan = ka_plan(b.T, b.n_seqs, p.G, H, D, b.max_pages);
   p.splits = plan.splits;
   const int dt = ka_dt(D);
   const bool qv = qdt == BL_BF16 && D % 32 == 0 && bl_aligned16(Q) && ldq % 8 == 0 && bl_aligned16(rope);

@@ -10,7 +10,7 @@ from tests.test_gpu_kv_attention import run
 pytestmark = pytest.mark.gpu
 
 # new, ctx, H, Hq, width of the page table
-FEW = ([300, 1, 77, 130], [100, 37, 0, 900], 8, 32, None)            # workgroups of 128 rows: of three sequences at most
+FEW = ([300, 1, 77, 130], [100, 37, 0, 900], 16, 64, None)           # workgroups of 128 rows: of three sequences at most
 MANY = ([500, 1, 523], [300, 700, 0], 16, 64, 20)                    # of 256 rows
 SETS = [FEW + (64,), FEW + (100,), FEW + (128,), FEW + (256,), MANY + (64,), MANY + (128,), MANY + (34,), MANY + (160,)]
 
