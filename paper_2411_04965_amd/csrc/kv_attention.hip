@@ -1362,12 +1362,13 @@ static KaPlan ka_plan(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t D
   return {(int)(want < most ? want : most), shift};
 }
 
-// Whole rows, up to 128 channels: eight waves of 32 rows (8), or of 16 (7) where 32 give less than a workgroup to every CU (4 sequences
-// of 256 on 2000 cached, 8 heads of 128: 59 us with 16, 88 with 32) or about one and the rows see very unlike numbers of pages, being
-// most of their sequences (4096 on none, 16 heads: 109 and 144; 2048 on 6144, 8 heads, the other way about: 281 and 254).
+// Whole rows, up to 128 channels: eight waves of 32 rows (8), whose turn of the chip takes 1.7 times that of eight waves of 16 (7).  Not
+// for a single turn where the new rows are most of their sequences and so see very unlike numbers of pages.  With 16 and 32: 4 sequences
+// of 256 x 4 rows on 2000 cached, 8 heads of 128: 59 and 88 us; 2048 x 4 on 6144, 281 and 254; 4096 on none, 16 heads, 109 and 144.
 static int ka_rows_shift(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t max_pages) {
-  const int64_t blocks = ka_tiles(T, G, n_seqs, 8) * H;
-  return blocks >= 512 || (blocks >= 256 && 2 * T <= n_seqs * max_pages * KP_TOKENS) ? 8 : 7;
+  const int64_t rows = (T * G + n_seqs - 1) / n_seqs;
+  auto turns = [&](int64_t unit) { return ((rows + unit - 1) / unit * n_seqs * H + 255) / 256; };
+  return 17 * turns(256) < 10 * turns(128) && (turns(256) > 1 || 2 * T <= n_seqs * max_pages * KP_TOKENS) ? 8 : 7;
 }
 
 size_t bl_kv_attention_ws_bytes(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t D, int64_t max_pages) {

@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 
 # new, ctx, H, Hq, width of the page table
 FEW = ([300, 1, 77, 130], [100, 37, 0, 900], 16, 64, None)           # workgroups of 128 rows: of three sequences at most
-MANY = ([500, 1, 523], [300, 700, 0], 16, 64, 20)                    # of 256 rows
+MANY = ([500, 1, 523], [300, 700, 0], 14, 56, 20)                    # of 256 rows: two turns of the chip with 128, one with 256
 SETS = [FEW + (64,), FEW + (100,), FEW + (128,), FEW + (256,), MANY + (64,), MANY + (128,), MANY + (34,), MANY + (160,)]
 
 
