@@ -73,7 +73,8 @@ __device__ __forceinline__ void rn_store16(float* x, int c, int K, const float (
 __device__ __forceinline__ float rn_round(float v, const uint16_t*) { return bl_bf16_to_f32(bl_f32_to_bf16_any(v)); }
 __device__ __forceinline__ float rn_round(float v, const float*) { return v; }
 
-// sum and maximum over a workgroup of NT threads, in every thread; `red` is used once a call
+// sum and maximum (of numbers that are not negative; a NaN is the largest) over a workgroup of NT threads, in every thread; `red` is
+// used once a call
 template <int NT>
 __device__ __forceinline__ double rn_sum(double v, double* red) {
   v = bl_wave_sum_f64_dpp(v);
@@ -86,15 +87,15 @@ __device__ __forceinline__ double rn_sum(double v, double* red) {
   return t;
 }
 template <int NT>
-__device__ __forceinline__ float rn_max(float v, float* red) {
-  v = __uint_as_float(bl_wave_max_u32(__float_as_uint(v)));
-  if (NT == 64) return v;
+__device__ __forceinline__ float rn_max(float x, u32* red) {
+  u32 v = bl_wave_max_u32(__float_as_uint(x) & 0x7FFFFFFFu);
+  if (NT == 64) return __uint_as_float(v);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
   v = red[0];
 #pragma unroll
-  for (int w = 1; w < NT / 64; ++w) v = fmaxf(v, red[w]);
-  return v;
+  for (int w = 1; w < NT / 64; ++w) v = max(v, red[w]);
+  return __uint_as_float(v);
 }
 
 enum { RN_INT4 = 0, RN_MX6 = 1, RN_INT8 = 2 };
@@ -112,7 +113,7 @@ __global__ __launch_bounds__(NT) void rmsnorm_quantize_kernel(const T* __restric
                                                               T* __restrict__ H, float* __restrict__ rstd_out,
                                                               u32* __restrict__ q_out, float* __restrict__ scale_out) {
   __shared__ double red0[NT / 64], red1[NT / 64];
-  __shared__ float redm[NT / 64];
+  __shared__ u32 redm[NT / 64];
   // block-ordered codes: tokens that share lines go to one XCD, as in the quantizer
   int64_t m = blockIdx.x;
   if (OUT == RN_MX6) {
@@ -148,7 +149,7 @@ __global__ __launch_bounds__(NT) void rmsnorm_quantize_kernel(const T* __restric
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       h[j][e] = (h[j][e] * rstd) * g[e];
-      if (OUT == RN_INT8) top = fmaxf(top, fabsf(h[j][e]));
+      if (OUT == RN_INT8) top = __builtin_elementwise_maximum(top, fabsf(h[j][e]));      // (a NaN stays, as in the quantizer)
       else sum += (double)fabsf(h[j][e]);
     }
   }
