@@ -46,22 +46,21 @@ __device__ __forceinline__ void kp_load8(const RawT* x, int c, int D, float (&v)
   }
 }
 
-// LPT lanes a token, 8 channels a lane
+// LPT lanes a token, 8 channels a lane.  A NaN is larger than any number, as where quantize_heads takes its maximum: it has to reach the scale.
 template <int LPT>
 __device__ __forceinline__ float kp_head_max(const float (&v)[8]) {
-  float m = 0.0f;
+  float f = 0.0f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[e]));
+  for (int e = 0; e < 8; ++e) f = __builtin_elementwise_maximum(f, fabsf(v[e]));
+  u32 m = __float_as_uint(f) & 0x7FFFFFFFu;
   // neighbours, pairs, then mirrored halves and rows, whose quads are alike by then
-  auto of = [](float x, auto ctrl) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xF, 0xF, false));
-  };
-  m = fmaxf(m, of(m, std::integral_constant<int, 0xB1>{}));
-  m = fmaxf(m, of(m, std::integral_constant<int, 0x4E>{}));
-  m = fmaxf(m, of(m, std::integral_constant<int, 0x141>{}));
-  if (LPT >= 16) m = fmaxf(m, of(m, std::integral_constant<int, 0x140>{}));
-  if (LPT >= 32) m = fmaxf(m, __shfl_xor(m, 16, 64));
-  return m;
+  auto of = [](u32 x, auto ctrl) { return (u32)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xF, 0xF, false); };
+  m = max(m, of(m, std::integral_constant<int, 0xB1>{}));
+  m = max(m, of(m, std::integral_constant<int, 0x4E>{}));
+  m = max(m, of(m, std::integral_constant<int, 0x141>{}));
+  if (LPT >= 16) m = max(m, of(m, std::integral_constant<int, 0x140>{}));
+  if (LPT >= 32) m = max(m, (u32)__shfl_xor((int)m, 16, 64));
+  return __uint_as_float(m);
 }
 
 // Levels RoundClip(v * s) of 8 channels, in nibbles: stored magnitude, sign (1: below zero), lowest magnitude bit of a 4-bit level.
