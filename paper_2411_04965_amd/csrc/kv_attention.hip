@@ -86,6 +86,15 @@ __device__ __forceinline__ float ka_max_groups(float v) {
   return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
 }
 
+// the same over the four lane groups for magnitudes, a NaN being the largest
+__device__ __forceinline__ float ka_top_groups(float v) {
+  const u32 b = __float_as_uint(v) & 0x7FFFFFFFu;
+  auto x = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  const u32 t = max((u32)x[0], (u32)x[1]);
+  x = __builtin_amdgcn_permlane16_swap(t, t, false, false);
+  return __uint_as_float(max((u32)x[0], (u32)x[1]));
+}
+
 __device__ __forceinline__ float ka_q_at(const KaArgs& p, int64_t at) {
   return p.q_f32 ? reinterpret_cast<const float*>(p.Q)[at] : bl_bf16_to_f32(reinterpret_cast<const uint16_t*>(p.Q)[at]);
 }
@@ -198,12 +207,15 @@ struct KaQuery {
 #pragma unroll
       for (int v = 0; v < 2; ++v)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[k][v][e]));
-    top = ka_max_groups(top);
+        for (int e = 0; e < 16; ++e) top = __builtin_elementwise_maximum(top, fabsf(x[k][v][e]));      // (a NaN stays)
+    top = ka_top_groups(top);
     const float lv = Q4 ? 7.0f : 15.0f;
     float f = Q4 ? 7.0f / (top + p.eps) : top > 0.0f ? 15.0f / top : 0.0f;
     if (!have) f = 0.0f;
     c = fmaxf(16.0f * p.cs * (top / lv), 1.17549435e-38f);      // digits are eighths, codes halves; never 0 (times -inf)
+    // A NaN or an infinity in the query: whatever its digits are, the largest score times this, less itself, is no number, and so are
+    // the row's sum and outputs.  What is not seen stays -inf: a row that sees nothing still has sum 0.
+    if (!(top < INFINITY)) c = INFINITY;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       u32 code[PARTS][32];
@@ -562,6 +574,9 @@ __device__ __forceinline__ void ka_walk(const KaArgs& p, const KvSeq& q, const K
   while (head) turn(std::false_type());
 }
 
+// What outputs are multiplied by (levels are halves): nothing seen, sum 0, gives zeros; a sum that is no number makes all outputs that.
+__device__ __forceinline__ float ka_inverse(float sum) { return sum == 0.0f ? 0.0f : 2.0f / sum; }
+
 template <int DT>
 __device__ __forceinline__ void ka_store(const KaArgs& p, const KvSeq& q, int r, int h, const v4f (&o)[DT / 16], float inv) {
   const int g = (threadIdx.x & 63) >> 4;
@@ -830,7 +845,7 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attention_wide_kernel(KaArgs
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     const int r = r0 + 16 * i + n;
-    if (r < rows) ka_store<DT>(p, q, r, h, st[i].o, l > 0.0f ? 2.0f / l : 0.0f);
+    if (r < rows) ka_store<DT>(p, q, r, h, st[i].o, ka_inverse(l));
   }
 }
 
@@ -1188,7 +1203,7 @@ __global__ __launch_bounds__(KR_THREADS) void kv_attention_rows_kernel(KaArgs p,
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     const int r = r0 + 16 * i + n;
-    if (r < rows) ka_store<DT>(p, q, r, h, st[i].o, l > 0.0f ? 2.0f / l : 0.0f);
+    if (r < rows) ka_store<DT>(p, q, r, h, st[i].o, ka_inverse(l));
   }
 }
 
@@ -1270,7 +1285,7 @@ __global__ __launch_bounds__(KA_THREADS, DT == 256 ? 1 : 2) void kv_attention_sp
       st.o[d][e] = v;
     }
   if (p.splits == 1) {
-    ka_store<DT>(p, q, r0 + n, h, st.o, sum > 0.0f ? 2.0f / sum : 0.0f);
+    ka_store<DT>(p, q, r0 + n, h, st.o, ka_inverse(sum));
     return;
   }
   float* part = p.part + ((item * p.H + h) * p.splits + split) * ka_part_floats(DT, R);
@@ -1328,7 +1343,7 @@ __global__ __launch_bounds__(KA_THREADS) void kv_attention_join_kernel(KaArgs p,
   __syncthreads();
   const int c = 2 * (int)threadIdx.x;
   if (c >= p.D) return;
-  const float inv = sum > 0.0f ? 2.0f / sum : 0.0f;
+  const float inv = ka_inverse(sum);
   float v[2];
 #pragma unroll
   for (int e = 0; e < 2; ++e) v[e] = (((lds_o[0][c + e] + lds_o[1][c + e]) + lds_o[2][c + e]) + lds_o[3][c + e]) * inv;
