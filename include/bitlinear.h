@@ -389,7 +389,8 @@ int kv_cache_read(const void* cache, const float* scales, int64_t pos0, int64_t 
  *   O          device, bfloat16 [T, Hq, D], dense, 16-byte aligned
  *   workspace  kv_pages_attention_workspace_bytes(T, n_seqs, Hq, H, D, max_pages) bytes, 16-byte aligned (may be 0: then NULL); what a
  *              call leaves there means nothing to the next, but calls that may overlap in time need one each
- *   Probabilities are rounded to 8 significand bits for the second product; sums, maxima and outputs are float32 until the end.
+ *   Probabilities times value scales are rounded to 8 significand bits for the second product (those below 2^-14 of the largest that the
+ *   row has in a page to 2^-22 of that); sums, maxima and outputs are float32 until the end.
  * Errors: BL_EINVAL (null pointer, enum, sizes < 1, Hq % H, scale not positive and finite, eps < 0, window or sinks < 0, strides),
  * BL_ESHAPE (D, n_pos, sizes), BL_EALIGN, BL_EWORKSPACE. */
 #define BL_KV_PAGE 128

@@ -11,8 +11,9 @@
 // of the largest channel.  6-bit x 4-bit products take half the time of 8-bit x 4-bit ones: three of them 51 cycles, two E4M3 parts (8
 // significand bits of every channel) 66.  4-bit queries (absmax, 7 levels) are one digit.
 //   Probabilities, times the value's scale, need relative precision: each is the sum of two E4M3 numbers, the second scaled by 2^-5,
-// which is one rounding to 8 significand bits, as bfloat16 operands would have it.  (Where many rows share a page the values widen to
-// bfloat16 and the probabilities are rounded to that instead.)
+// which is one rounding to 8 significand bits, as bfloat16 operands would have it, down to 2^-14 of the query's largest in the page; what
+// is smaller ends at 2^-22 of that.  (Where many rows share a page the values widen to bfloat16 and the probabilities are rounded to that
+// instead.)
 // Products are exact, sums float32.
 //
 // Keys are the row operand, queries the column operand: a lane ends up with the scores of one query against 4 consecutive tokens
@@ -303,38 +304,46 @@ __device__ __forceinline__ void ka_load_keys(const unsigned char* head, int U, K
 template <int DT>
 __device__ __forceinline__ KaWords ka_load_values(const unsigned char* head, int U, int d) {
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-  const int ch = min(16 * d, 32 * U - 16) + n;      // (channels that the head lacks are not stored)
-  return *reinterpret_cast<const KaWords*>(head + kp_code_bytes(U) + (u32)(ch * 4 + g) * 12);
+  // (channels that the head lacks are not stored; the group's place is the same for the wave: one offset register for all groups)
+  return *reinterpret_cast<const KaWords*>(head + (kp_code_bytes(U) + 48 * min(16 * d, 32 * U - 16)) + (u32)(n * 4 + g) * 12);
 }
 
 // a * b, and 0 where either is 0, whatever the other is (the instruction, so that the compiler knows of it)
 extern "C" __device__ float ka_mul_legacy(float a, float b) __asm("llvm.amdgcn.fmul.legacy");
 
-// Probabilities of 16 queries as the second product's operands; scales(t): the four value scales of scores t.  What is not seen has
-// probability 0, and 0 times a scale that is infinite or no number is 0 here.
+// E of a largest weight: weights times ka_scale_factor(E) = 2^(134 - E) are below 2^8, E - 7 is the E8M0 of what that took away
+__device__ __forceinline__ int ka_exponent(float top) { return min(max((int)(__float_as_uint(top) >> 23), 16), 254); }
+__device__ __forceinline__ float ka_scale_factor(int E) { return __uint_as_float((u32)(261 - E) << 23); }
+
+// Weights p * scale of 16 queries as the second product's operands; scales(t): the four value scales of scores t.  What is not seen has
+// probability 0, and 0 times a scale that is infinite or no number is 0 here.  They are brought below 2^8 by a power of two that the
+// instruction puts back: that of the column's largest weight in the page, not of its largest scale, for a key of next to no weight may be
+// all that has a value.  -> E, its exponent (ka_exponent)
 template <int N, typename F>
-__device__ __forceinline__ void ka_weights(const v4f (&S)[N], F scales, float c, float base, float& l, int (&ph)[N], int (&pl)[N]) {
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+__device__ __forceinline__ int ka_weights(v4f (&S)[N], F scales, float c, float base, float& l, int (&ph)[N], int (&pl)[N]) {
+  float sum[4] = {0.f, 0.f, 0.f, 0.f}, top = 0.0f;
 #pragma unroll
   for (int t = 0; t < N; ++t) {
     const float4 s4 = scales(t);
     const float vs[4] = {s4.x, s4.y, s4.z, s4.w};
-    float w[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t][r], c, -base));
       sum[r] += e;
-      w[r] = ka_mul_legacy(e, vs[r]);
+      S[t][r] = ka_mul_legacy(e, vs[r]);
     }
-    ka_split4(w, __float_as_int(S[t][0]), ph[t], pl[t]);
+    top = ka_max3(ka_max3(top, S[t][0], S[t][1]), S[t][2], S[t][3]);
   }
   l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  const int E = ka_exponent(ka_max_groups(top));
+  const float f = ka_scale_factor(E);
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    const float w[4] = {S[t][0] * f, S[t][1] * f, S[t][2] * f, S[t][3] * f};
+    ka_split4(w, __float_as_int(w[0]), ph[t], pl[t]);
+  }
+  return E;
 }
-// a scale as far as it counts for E: one that is infinite or no number may belong to a place that some rows do not see
-__device__ __forceinline__ float ka_finite(float s) { return __float_as_uint(s) < 0x7F800000u ? s : 0.0f; }
-// E of a largest value scale: scales times ka_scale_factor(E) = 2^(134 - E) are below 2^8, E - 7 is the E8M0 of what that took away
-__device__ __forceinline__ int ka_exponent(float top) { return min(max((int)(__float_as_uint(top) >> 23), 16), 254); }
-__device__ __forceinline__ float ka_scale_factor(int E) { return __uint_as_float((u32)(261 - E) << 23); }
 
 // Operands of the first token's lowest magnitude bits (nibble 1 = half a level, of the sign in C): 32 channels of the key ...
 __device__ __forceinline__ void ka_low_keys(u32 low, u32 C, u32 (&a)[4]) {
@@ -480,36 +489,12 @@ __device__ __forceinline__ void ka_page(const KaArgs& p, const KaRange& rg, int 
     for (int r = 0; r < 4; ++r) S[t][r] *= w.ks[t][r];
   ka_load_scales<STEP>(next_scale, base_tok, w.ks);
   const int64_t t0 = (int64_t)page * KP_TOKENS;
-  float vm = 0.0f;
-  if (ka_masked(p, rg, t0)) {
-    ka_mask<STEP>(S, KaSeen(p, t0, qy.pos, qy.pos, base_tok));
-    KaSeen any(p, t0, rg.min_pos, rg.max_pos, base_tok);        // places that no query of the wave sees may hold anything
-    asm volatile("" : "+v"(any.hi), "+v"(any.lo), "+v"(any.snk));
-#pragma unroll
-    for (int t = 0; t < N; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        w.vs[t][r] = any.at(ka_token(STEP * t, r)) ? w.vs[t][r] : 0.0f;
-        vm = fmaxf(vm, ka_finite(w.vs[t][r]));
-      }
-  } else {
-#pragma unroll
-    for (int t = 0; t < N; ++t) vm = ka_max3(ka_max3(vm, w.vs[t][0], w.vs[t][1]), w.vs[t][2], w.vs[t][3]);
-  }
-
-  // value scales, brought below 2^8 by a power of two 2^(E - 134) that the instruction puts back
-  vm = ka_max_groups<R>(vm);
-  const int E = ka_exponent(vm);
-  const float vf = ka_scale_factor(E);
-#pragma unroll
-  for (int t = 0; t < N; ++t)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) w.vs[t][r] *= vf;
+  if (ka_masked(p, rg, t0)) ka_mask<STEP>(S, KaSeen(p, t0, qy.pos, qy.pos, base_tok));
 
   const float base = ka_rescale<DT, R>(S, qy.c, st);
   int wh[N], wl[N];
   auto scales = [&](int t) { return make_float4(w.vs[t][0], w.vs[t][1], w.vs[t][2], w.vs[t][3]); };
-  ka_weights(S, scales, qy.c, base, st.l, wh, wl);
+  const int E = ka_weights(S, scales, qy.c, base, st.l, wh, wl);
   ka_load_scales<STEP>(next_scale + KP_TOKENS, base_tok, w.vs);
   v8i ph, pl;
 #pragma unroll
@@ -517,6 +502,8 @@ __device__ __forceinline__ void ka_page(const KaArgs& p, const KaRange& rg, int 
     ph[t] = STEP == 1 || j == t % STEP ? wh[t / STEP] : 0;
     pl[t] = STEP == 1 || j == t % STEP ? wl[t / STEP] : 0;
   }
+  // (the scheduler would widen values above, between the weights, and fetch the next page's later for it: 131072 keys 33 us, 31 so)
+  __builtin_amdgcn_sched_barrier(0);
 
 #pragma unroll
   for (int d = 0; d < DT / 16; ++d) {
@@ -614,7 +601,6 @@ struct KaStage {
   static constexpr int VT = DT / 16;                     // and of value operands
   uint4 keys[KT * 64], vals[VT * 64];
   float ks[KP_TOKENS], vs[KP_TOKENS];
-  int E[4];                                              // of tokens 0 .. 63, of tokens 64 .. 127
 };
 template <int DT>
 struct KaRaw {                                           // a wave's share of a page on its way
@@ -641,7 +627,7 @@ __device__ __forceinline__ void ka_fetch(const unsigned char* head, int U, int w
 }
 
 template <int DT>
-__device__ __forceinline__ void ka_widen(const KaArgs& p, const KaRange& rg, int page, int wave, const KaRaw<DT>& raw, KaStage<DT>& to) {
+__device__ __forceinline__ void ka_widen(int page, int wave, const KaRaw<DT>& raw, KaStage<DT>& to) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int i = 0; i < KaStage<DT>::KT / 4; ++i) {
@@ -661,12 +647,7 @@ __device__ __forceinline__ void ka_widen(const KaArgs& p, const KaRange& rg, int
     to.ks[threadIdx.x] = s;
   } else {
     const int tok = (int)threadIdx.x - KP_TOKENS;
-    if (page == 0 && tok == 0) s *= 2.0f;
-    // places that no row of the workgroup sees may hold anything
-    if (!KaSeen(p, (int64_t)page * KP_TOKENS, rg.min_pos, rg.max_pos, 0).at(tok)) s = 0.0f;
-    const int E = ka_exponent(__uint_as_float(bl_wave_max_u32(__float_as_uint(ka_finite(s)))));
-    to.vs[tok] = s * ka_scale_factor(E);
-    if (lane == 0) to.E[wave - 2] = E;
+    to.vs[tok] = page == 0 && tok == 0 ? 2.0f * s : s;
   }
 }
 
@@ -729,6 +710,7 @@ __device__ __forceinline__ void ka_staged(const KaArgs& p, const KaRange& rg, in
   }
   const bool masked = ka_masked(p, rg, t0);
   v8i ph[QT], pl[QT];
+  int E[QT];
   auto scales = [&](int t) { return *reinterpret_cast<const float4*>(sg.vs + 16 * g + ka_token(t, 0)); };
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
@@ -736,7 +718,7 @@ __device__ __forceinline__ void ka_staged(const KaArgs& p, const KaRange& rg, in
     const float base = ka_rescale<DT, 16>(S[i], qc[i], st[i]);
     __builtin_amdgcn_sched_barrier(0);
     int wh[8], wl[8];
-    ka_weights(S[i], scales, qc[i], base, st[i].l, wh, wl);
+    E[i] = ka_weights(S[i], scales, qc[i], base, st[i].l, wh, wl);
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
       ph[i][t] = wh[t];
@@ -745,7 +727,6 @@ __device__ __forceinline__ void ka_staged(const KaArgs& p, const KaRange& rg, in
     asm volatile("" : "+v"(ph[i]), "+v"(pl[i]), "+v"(st[i].l));      // (done here, not where it is used)
     __builtin_amdgcn_sched_barrier(0);
   }
-  const int E = sg.E[g >> 1];          // (the instruction's scale of 32 tokens is that of their lane group)
   ahead = sg.vals[lane];
 #pragma unroll
   for (int d = 0; d < DT / 16; ++d) {
@@ -753,8 +734,8 @@ __device__ __forceinline__ void ka_staged(const KaArgs& p, const KaRange& rg, in
     if (d + 1 < DT / 16) ahead = sg.vals[64 * (d + 1) + lane];
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
-      st[i].o[d] = ka_mfma_pv(a, ph[i], st[i].o[d], 127, E - 7);
-      st[i].o[d] = ka_mfma_pv(a, pl[i], st[i].o[d], 127, E - 12);
+      st[i].o[d] = ka_mfma_pv(a, ph[i], st[i].o[d], 127, E[i] - 7);
+      st[i].o[d] = ka_mfma_pv(a, pl[i], st[i].o[d], 127, E[i] - 12);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -766,8 +747,8 @@ __device__ __forceinline__ void ka_staged(const KaArgs& p, const KaRange& rg, in
       ka_low_values(lows, U, d, reinterpret_cast<const u32*>(head + kp_code_bytes(U))[ch * 12 + 2], a);
 #pragma unroll
       for (int i = 0; i < QT; ++i) {
-        st[i].o[d] = ka_mfma_pv(a, ph[i], st[i].o[d], 126, E - 7);
-        st[i].o[d] = ka_mfma_pv(a, pl[i], st[i].o[d], 126, E - 12);
+        st[i].o[d] = ka_mfma_pv(a, ph[i], st[i].o[d], 126, E[i] - 7);
+        st[i].o[d] = ka_mfma_pv(a, pl[i], st[i].o[d], 126, E[i] - 12);
       }
     }
   }
@@ -821,7 +802,7 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attention_wide_kernel(KaArgs
   const unsigned char* head = ka_next(p, q, all, h, hb, 1, k, page);
   if (head) {
     ka_fetch<DT>(head, U, wave, raw);
-    ka_widen<DT>(p, all, page, wave, raw, stage[0]);
+    ka_widen<DT>(page, wave, raw, stage[0]);
   }
   __syncthreads();
   auto turn = [&](auto first) __attribute__((always_inline)) {
@@ -831,7 +812,7 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attention_wide_kernel(KaArgs
     if (next) ka_fetch<DT>(next, U, wave, raw);
     ka_staged<decltype(first)::value, DT, QT, Q4, QV>(p, rg, page, head, U, stage[cur], digits, qc, qp, st);
     // the other buffer was last read a page ago, before the barrier that ended it
-    if (next) ka_widen<DT>(p, all, page2, wave, raw, stage[cur ^ 1]);
+    if (next) ka_widen<DT>(page2, wave, raw, stage[cur ^ 1]);
     __syncthreads();
     head = next;
     page = page2;
