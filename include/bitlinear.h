@@ -382,6 +382,8 @@ int kv_cache_read(const void* cache, const float* scales, int64_t pos0, int64_t 
  * kv_pages_attention: O[t] = sum_j p_j v_j / sum_j p_j over the visible positions j of the row's sequence, p_j = exp(scale * q . k_j)
  *   relative to the largest; position j is visible to a row at position i if j <= i, and, where window > 0, j > i - window or
  *   j < sinks.  A row that sees nothing (or only absent pages) gives zeros.
+ *   NaN and infinities: a row whose query holds one, or that sees a key or a value whose scale is not finite, gives NaN in all channels;
+ *   what stands in places that a row does not see means nothing to it.
  *   Q          device [T, Hq, D] of q_dtype, row t at element t * ldq, aligned to its elements; Hq a multiple of H: query head h reads head
  *              h / (Hq / H)
  *   q_bits     16: queries as they are (rotated, every channel kept to 1 / 7680 of the row's largest); 4: quantize_heads' 4-bit levels of

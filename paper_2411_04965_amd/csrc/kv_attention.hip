@@ -418,6 +418,12 @@ __device__ __forceinline__ float ka_rescale(const v4f (&S)[N], float c, KaState<
   return base;
 }
 
+// A state that is not finite makes every row that sees it no number, as the formula does, whatever the sign of the product with an
+// infinite key, and however small the weight of a value: the score is NaN for either.
+__device__ __forceinline__ float ka_poison(float s, float v) {
+  return fabsf(s) < INFINITY && fabsf(v) < INFINITY ? s : __uint_as_float(0x7FC00000u);
+}
+
 // A lane's scales: those of its scores' tokens
 template <int STEP, int N>
 __device__ __forceinline__ void ka_load_scales(const float* s, int base, float (&v)[N][4]) {
@@ -489,7 +495,24 @@ __device__ __forceinline__ void ka_page(const KaArgs& p, const KaRange& rg, int 
     for (int r = 0; r < 4; ++r) S[t][r] *= w.ks[t][r];
   ka_load_scales<STEP>(next_scale, base_tok, w.ks);
   const int64_t t0 = (int64_t)page * KP_TOKENS;
-  if (ka_masked(p, rg, t0)) ka_mask<STEP>(S, KaSeen(p, t0, qy.pos, qy.pos, base_tok));
+  float odd = 0.0f;
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      odd = __builtin_elementwise_maximum(odd, __builtin_elementwise_maximum(fabsf(S[t][r]), fabsf(w.vs[t][r])));
+  u32 bits = __float_as_uint(odd);
+  asm("" : "+v"(bits));                    // (floats compared under a vote: this compiler lets a NaN pass as less than infinity)
+  const bool finite = __all((bits & 0x7FFFFFFFu) < 0x7F800000u);
+  if (ka_masked(p, rg, t0) || !finite) {
+    if (!finite) {
+#pragma unroll
+      for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[t][r] = ka_poison(S[t][r], w.vs[t][r]);
+    }
+    ka_mask<STEP>(S, KaSeen(p, t0, qy.pos, qy.pos, base_tok));
+  }
 
   const float base = ka_rescale<DT, R>(S, qy.c, st);
   int wh[N], wl[N];
@@ -605,7 +628,7 @@ struct KaStage {
 template <int DT>
 struct KaRaw {                                           // a wave's share of a page on its way
   KaWords k[KaStage<DT>::KT / 4], v[KaStage<DT>::VT / 4];
-  float scale;
+  float scale, value;                                    // value: for waves 0, 1 the value scale of the key's token
 };
 
 template <int DT>
@@ -623,7 +646,9 @@ __device__ __forceinline__ void ka_fetch(const unsigned char* head, int U, int w
     const int ch = min(16 * (4 * i + wave), 32 * U - 16) + n;
     raw.v[i] = *reinterpret_cast<const KaWords*>(v + (u32)(ch * 4 + g) * 12);
   }
-  raw.scale = reinterpret_cast<const float*>(head + kp_scale_off(U))[threadIdx.x];       // waves 0, 1: keys; 2, 3: values
+  const float* s = reinterpret_cast<const float*>(head + kp_scale_off(U));
+  raw.scale = s[threadIdx.x];                            // waves 0, 1: keys; 2, 3: values
+  raw.value = s[threadIdx.x | KP_TOKENS];
 }
 
 template <int DT>
@@ -644,7 +669,7 @@ __device__ __forceinline__ void ka_widen(int page, int wave, const KaRaw<DT>& ra
   float s = raw.scale;
   if (wave < 2) {
     if (page == 0 && threadIdx.x == 0) s *= 2.0f;
-    to.ks[threadIdx.x] = s;
+    to.ks[threadIdx.x] = ka_poison(s, raw.value);
   } else {
     const int tok = (int)threadIdx.x - KP_TOKENS;
     to.vs[tok] = page == 0 && tok == 0 ? 2.0f * s : s;
@@ -856,7 +881,7 @@ struct KrScales {
 };
 struct KrRaw {                              // a wave's share of a bundle on its way
   KaWords k, v;
-  float s;
+  float s, value;                           // value: for waves 0, 1 the value scale of the key's token
 };
 template <int DT, int QT, bool Q4, bool QV>
 struct KrShared {
@@ -878,6 +903,7 @@ __device__ __forceinline__ void kr_fetch(const unsigned char* pk, const unsigned
   if (DT == 128 || wave >= 4) raw.k = kr_fetch_keys<DT>(pk, U, DT == 64 ? wave - 4 : wave);
   if (DT == 128 || wave < 4) raw.v = ka_load_values<DT>(pv, U, wave);
   if (wave < 4) raw.s = reinterpret_cast<const float*>(pk + kp_scale_off(U))[threadIdx.x];      // waves 0, 1: keys'; 2, 3: values'
+  if (wave < 2) raw.value = reinterpret_cast<const float*>(pk + kp_scale_off(U))[threadIdx.x + KP_TOKENS];
 }
 template <int DT>
 __device__ __forceinline__ void kr_widen_keys(const KaWords& w, int piece, KrBundle<DT>& to) {
@@ -905,9 +931,10 @@ __device__ __forceinline__ void kr_first_value(const KaWords& w, int d, const u3
   if (lane < 16) reinterpret_cast<uint16_t*>(to.vals + d * 256 + lane)[0] = (uint16_t)(__float_as_uint(w.c & 8u ? -m : m) >> 16);
 }
 // a page's scales as its rows take them: no value weight where no row of the workgroup sees the place, whatever stands there
-__device__ __forceinline__ void kr_scale(const KaArgs& p, const KaRange& all, int page, int wave, float s, KrScales& to) {
+__device__ __forceinline__ void kr_scale(const KaArgs& p, const KaRange& all, int page, int wave, const KrRaw& raw, KrScales& to) {
+  const float s = raw.s;
   if (wave < 2) {
-    to.k[threadIdx.x] = page == 0 && threadIdx.x == 0 ? 2.0f * s : s;
+    to.k[threadIdx.x] = ka_poison(page == 0 && threadIdx.x == 0 ? 2.0f * s : s, raw.value);
   } else {
     const int tok = (int)threadIdx.x - KP_TOKENS;
     to.v[tok] = KaSeen(p, (int64_t)page * KP_TOKENS, all.min_pos, all.max_pos, 0).at(tok) ? s : 0.0f;
@@ -1022,11 +1049,11 @@ __global__ __launch_bounds__(KR_THREADS) void kv_attention_rows_kernel(KaArgs p,
       kp_expand(raw.v.a, raw.v.b, raw.v.c, o);
 #pragma unroll
       for (int v = 0; v < 4; ++v) values(v, o, sh.bundle[0]);
-      if (wave < 4) kr_scale(p, all, page[0], wave, raw.s, sh.scales[0]);
+      if (wave < 4) kr_scale(p, all, page[0], wave, raw, sh.scales[0]);
     }
     kr_fetch<DT>(head[1] ? head[1] : head[0], head[0], U, wave, raw);
     if (has_k) kr_widen_keys<DT>(raw.k, kp, sh.bundle[0]);
-    if (wave < 4) kr_scale(p, all, page[1], wave, raw.s, sh.scales[1]);
+    if (wave < 4) kr_scale(p, all, page[1], wave, raw, sh.scales[1]);
     kr_fetch<DT>(head[2] ? head[2] : head[0], head[0], U, wave, raw);
     __syncthreads();
     kr_digits(digits, dg);
@@ -1107,7 +1134,7 @@ __global__ __launch_bounds__(KR_THREADS) void kv_attention_rows_kernel(KaArgs p,
         for (int i = 0; i < QT; ++i)
 #pragma unroll
           for (int d = 0; d < DT / 16; ++d) asm volatile("" : "+v"(st[i].o[d]));
-        if (wave < 4) kr_scale(p, all, page[2], wave, raw.s, sh.scales[(turn + 2) & 3]);
+        if (wave < 4) kr_scale(p, all, page[2], wave, raw, sh.scales[(turn + 2) & 3]);
         if (page[0] == 0 && has_v) kr_first_value<DT>(first, wave, reinterpret_cast<const u32*>(head[0] + kp_low_off(U)), U, to);
       }
       kr_fetch<DT>(head[3] ? head[3] : head[0], head[1] ? head[1] : head[0], U, wave, raw);

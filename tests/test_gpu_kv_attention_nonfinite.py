@@ -64,3 +64,45 @@ def test_such_a_query_that_sees_nothing():
         Q[0], Q[b.T - 1] = float("nan"), float("inf")
         out = attend(b, Q)
         assert bool((out[:2] == 0).all()) and bool((out[new[0]:] == 0).all()) and bool(torch.isfinite(out).all())
+
+
+def spoiled(b, at, key=None, value=None, head=0):
+    """The scale of head 0 at position `at` of sequence 0 in the pool's bytes."""
+    n = b.pool.n_codes
+    f = b.pool.floats[b.table[0, at // 128], head]
+    if key is not None:
+        f[2 * n + at % 128] = key
+    if value is not None:
+        f[2 * n + 128 + at % 128] = value
+
+
+@pytest.mark.parametrize("key,value", [(np.nan, None), (np.inf, None), (None, np.nan), (None, np.inf)])
+@pytest.mark.parametrize("form", FORMS, ids=IDS)
+def test_a_state_that_is_not_finite(form, key, value):
+    b, Hq = batch(form, 83)
+    Q, G = queries(b, Hq), Hq // b.H
+    n0, ctx = b.new[0], form[1][0]
+    for at in (0, ctx + n0 - 1 - n0 // 3):                           # the sequence's first state, and one of the new rows'
+        kept = b.pool.raw.copy()
+        clean = attend(b, Q)
+        spoiled(b, at, key, value)
+        out = attend(b, Q)
+        b.pool.raw[:] = kept
+        bad = torch.zeros(b.T, Hq, dtype=torch.bool, device="cuda")
+        bad[max(at - ctx, 0):n0, :G] = True                          # the rows of sequence 0 that see it
+        assert bool(torch.isnan(out[bad]).all()), at
+        assert torch.equal(out[~bad], clean[~bad]), at
+
+
+@pytest.mark.parametrize("form", FORMS, ids=IDS)
+def test_whatever_the_weight_or_the_values(form):
+    """A value of next to no weight, a key beside values that are all zero."""
+    b, Hq = batch(form, 84)
+    Q, n0, G = queries(b, Hq) * 50, b.new[0], Hq // b.H
+    spoiled(b, 1 if form[1][0] else 0, value=np.nan)
+    assert bool(torch.isnan(attend(b, Q)[:n0, :G]).all())
+    n = b.pool.n_codes
+    b.fill()
+    b.pool.floats[b.table[0, 0], 0, 2 * n + 128:2 * n + 256] = 0.0
+    spoiled(b, 0, key=np.nan)
+    assert bool(torch.isnan(attend(b, Q)[:n0, :G]).all())
