@@ -1029,6 +1029,7 @@ __global__ __launch_bounds__(QA_THREADS) void quant_fp4_mx_kernel(const uint16_t
 }
 
 // ---------------------------------------------------------------- format helper
+// FP4 codes, a channel a thread (the INT modes: unpack_act16_kernel)
 __global__ __launch_bounds__(QA_THREADS) void unpack_act_kernel(const u32* __restrict__ q, int mode,
                                                                 int64_t M, int K, int Kp,
                                                                 int8_t* __restrict__ codes) {
@@ -1037,34 +1038,7 @@ __global__ __launch_bounds__(QA_THREADS) void unpack_act_kernel(const u32* __res
   const int64_t m = id / K;
   const int k = (int)(id % K);
   int v;
-  if (mode == BL_ACT_INT4_ABSMEAN) {
-    const u32 word = q[m * (Kp / 8) + (k >> 3)];
-    const int kk = k & 7;
-    const u32 nibv = (word >> (8 * (kk & 3) + 4 * (kk >> 2))) & 15u;
-    v = (int)(nibv << 28) >> 28;
-  } else if (mode == BL_ACT_TOPK_INT8_ABSMAX) {
-    const u32 word = q[m * (Kp / 4) + (k >> 2)];
-    v = (int)(int8_t)((word >> (8 * (k & 3))) & 255u);
-  } else if (mode == BL_ACT_INT4_ABSMEAN_MX6) {
-    // value i of unit u: bits 6 i .. 6 i + 5 of the unit's stream, bytes 0..15 in the P piece and
-    // bytes 16..23 in the Q piece of the token's row inside its 32-token block
-    const unsigned char* blk = reinterpret_cast<const unsigned char*>(q) +
-                               ((m >> 5) * (int64_t)(Kp / 128) + (k >> 7)) * 3072;
-    const int r = (int)(m & 31), u = (k >> 5) & 3, bit = 6 * (k & 31);
-    const unsigned char* pp = blk + r * 64 + ((u ^ ((r >> 2) & 3)) << 4);
-    const unsigned char* qq = blk + 2048 + r * 32 + ((u ^ ((r >> 3) & 3)) << 3);
-    u32 two = 0;                                            // the two stream bytes that hold the code
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int byte = (bit >> 3) + j;
-      if (byte < 24) two |= (u32)(byte < 16 ? pp[byte] : qq[byte - 16]) << (8 * j);
-    }
-    const u32 c = (two >> (bit & 7)) & 63u;
-    const int e = (int)((c >> 2) & 7u), mant = (int)(c & 3u);
-    // levels are integers: 2^(e-3) * (1 + mant/4) for e >= 1, zero otherwise
-    const int mag = e == 0 ? 0 : (((4 + mant) << e) >> 5);
-    v = (c & 32u) ? -mag : mag;
-  } else if (mode == BL_ACT_FP4_E2M1_B32_MX) {
+  if (mode == BL_ACT_FP4_E2M1_B32_MX) {
     const unsigned char* blk = reinterpret_cast<const unsigned char*>(q) +
                                ((m >> 5) * (int64_t)(Kp / 128) + (k >> 7)) * 2048;
     const int r = (int)(m & 31), u = (k >> 5) & 3, i = k & 31;
@@ -1339,6 +1313,7 @@ __global__ __launch_bounds__(QA_THREADS) void unpack_act16_kernel(const u32* __r
         const int bit = 6 * j;
         u32 c = w3[bit >> 5] >> (bit & 31);
         if ((bit & 31) > 26) c |= w3[(bit >> 5) + 1] << (32 - (bit & 31));
+        // (levels are integers: 2^(e - 3) (1 + mantissa / 4) for e >= 1, else zero)
         const int e = (int)((c >> 2) & 7u), mag = e == 0 ? 0 : (int)(((4 + (c & 3u)) << e) >> 5);
         o[j >> 2] |= (u32)((c & 32u ? -mag : mag) & 255) << (8 * (j & 3));
       }
