@@ -386,7 +386,7 @@ int kv_cache_read(const void* cache, const float* scales, int64_t pos0, int64_t 
  *   what stands in places that a row does not see means nothing to it.
  *   Q          device [T, Hq, D] of q_dtype, row t at element t * ldq, aligned to its elements; Hq a multiple of H: query head h reads head
  *              h / (Hq / H)
- *   q_bits     16: queries as they are (rotated, every channel kept to 1 / 7680 of the row's largest); 4: quantize_heads' 4-bit levels of
+ *   q_bits     16: queries as they are (rotated, every channel kept to 1 / 30720 of the row's largest); 4: quantize_heads' 4-bit levels of
  *              the rotated query (Table 3's 4-bit Q), eps its epsilon
  *   O          device, bfloat16 [T, Hq, D], dense, 16-byte aligned
  *   workspace  kv_pages_attention_workspace_bytes(T, n_seqs, Hq, H, D, max_pages) bytes, 16-byte aligned (may be 0: then NULL); what a

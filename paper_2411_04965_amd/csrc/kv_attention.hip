@@ -6,10 +6,10 @@
 // Both products run on the block-float instruction 16 x 16 x 128, which contracts over a page's 128 tokens.  The cache's codes are
 // sign and two magnitude bits: the nibble of the E2M1 value code / 2, so 32 codes widen to an operand with 11 shifts and masks and
 // are exact.
-//   Queries are fixed-point numbers of the row's largest channel: three digits -15 .. 15, -8 .. 8, -8 .. 8 in E2M3 (whose codes 0 ..
-// 15 are the values 0 .. 15 eighths), a sixteenth apart through the instruction's scale operand; what is lost is at most 1 / 7680
-// of the largest channel.  6-bit x 4-bit products take half the time of 8-bit x 4-bit ones: three of them 51 cycles, two E4M3 parts (8
-// significand bits of every channel) 66.  4-bit queries (absmax, 7 levels) are one digit.
+//   Queries are sums of three E2M3 numbers, a sixteenth apart through the instruction's scale operand: with the row's largest channel at
+// 7.5, the first leaves at most a quarter, the second, of that times 16, an eighth of its unit, the third half of its smallest step:
+// 1 / 30720 of the largest channel is lost.  6-bit x 4-bit products take half the time of 8-bit x 4-bit ones: three of them 51 cycles, two
+// E4M3 parts (8 significand bits of every channel) 66.  4-bit queries (absmax, 7 levels) are one digit, in eighths.
 //   Probabilities, times the value's scale, need relative precision: each is the sum of two E4M3 numbers, the second scaled by 2^-5,
 // which is one rounding to 8 significand bits, as bfloat16 operands would have it, down to 2^-14 of the query's largest in the page; what
 // is smaller ends at 2^-22 of that.  (Where many rows share a page the values widen to bfloat16 and the probabilities are rounded to that
@@ -112,6 +112,23 @@ __device__ __forceinline__ void ka_bf16x16(const uint4 (&w)[2], float (&x)[16]) 
   }
 }
 
+// 32 channels, even and odd, as E2M3 codes in order: the nearest to x / unit (a power of two), and the way back.
+// (Written out because the results must not share registers with arguments: the builtins let them, and the last channels, read after
+// the first results are written, then come out wrong.)
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef float v32f __attribute__((ext_vector_type(32)));
+typedef u32 v6u __attribute__((ext_vector_type(6)));
+__device__ __forceinline__ v6u ka_pack6(v16f even, v16f odd, float unit) {
+  v6u w;
+  asm("v_cvt_scalef32_2xpk16_fp6_f32 %0, %1, %2, %3\n\ts_nop 1" : "=&v"(w) : "v"(even), "v"(odd), "v"(unit));
+  return w;
+}
+__device__ __forceinline__ v32f ka_unpack6(v6u w, float unit) {
+  v32f x;
+  asm("v_cvt_scalef32_pk32_f32_fp6 %0, %1, %2\n\ts_nop 1" : "=&v"(x) : "v"(w), "v"(unit));
+  return x;
+}
+
 // One query's operands: lane group g holds the digits of channels 32 g .. 32 g + 31 of every 128.  DT = 64: the second half of the
 // contraction takes the second digit against the same codes, so two instructions do.
 // QV: bfloat16 rows at 16-byte boundaries with D % 32 == 0 (16 channels then lie in one half of the rotation's pairs): all loads of a
@@ -210,40 +227,49 @@ struct KaQuery {
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = __builtin_elementwise_maximum(top, fabsf(x[k][v][e]));      // (a NaN stays)
     top = ka_top_groups(top);
-    const float lv = Q4 ? 7.0f : 15.0f;
-    float f = Q4 ? 7.0f / (top + p.eps) : top > 0.0f ? 15.0f / top : 0.0f;
+    // digits are E2M3 values up to 7.5 (4-bit levels: eighths), codes halves; c is never 0 (times -inf)
+    float f = Q4 ? 7.0f / (top + p.eps) : top > 0.0f ? 7.5f / top : 0.0f;
     if (!have) f = 0.0f;
-    c = fmaxf(16.0f * p.cs * (top / lv), 1.17549435e-38f);      // digits are eighths, codes halves; never 0 (times -inf)
+    c = fmaxf(16.0f * p.cs * (top / (Q4 ? 7.0f : 60.0f)), 1.17549435e-38f);
     // A NaN or an infinity in the query: whatever its digits are, the largest score times this, less itself, is no number, and so are
     // the row's sum and outputs.  What is not seen stays -inf: a row that sees nothing still has sum 0.
     if (!(top < INFINITY)) c = INFINITY;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
-      u32 code[PARTS][32];
+      v16f a, b;                           // even and odd channels
 #pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        // magnitude in 256ths of a unit: the digits are its three nibbles, the sign is theirs alike
-        const float y = x[k][e >> 4][e & 15] * f;
-        const u32 sg = (__float_as_uint(y) >> 26) & 32u;
-        const u32 m = Q4 ? (u32)fminf(rintf(fabsf(y)), 7.0f) << 8 : (u32)fminf(rintf(fabsf(y) * 256.0f), 3840.0f);
-        u32 d[3] = {m >> 8, (m >> 4) & 15u, m & 15u};
-        if (DT == 64) {
-          if (g >= 2) { d[0] = Q4 ? 0u : d[1]; d[1] = 0u; } else d[1] = d[2];
+      for (int e = 0; e < 16; ++e) {
+        a[e] = x[k][e >> 3][2 * (e & 7)] * f;
+        b[e] = x[k][e >> 3][2 * (e & 7) + 1] * f;
+        if (Q4) {
+          a[e] = fminf(fmaxf(rintf(a[e]), -7.0f), 7.0f);
+          b[e] = fminf(fmaxf(rintf(b[e]), -7.0f), 7.0f);
         }
+      }
+      v6u w[3];
+      if (Q4) {
+        w[0] = ka_pack6(a, b, 8.0f);
+      } else {
 #pragma unroll
-        for (int w = 0; w < PARTS; ++w) code[w][e] = d[w] | sg;
+        for (int d = 0; d < 3; ++d) {      // each digit is the nearest to what the ones before it leave
+          const float unit = d == 0 ? 1.0f : d == 1 ? 0.0625f : 0.00390625f;
+          w[d] = ka_pack6(a, b, unit);
+          if (d == 2) break;
+          const v32f y = ka_unpack6(w[d], unit);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            a[e] -= y[2 * e];
+            b[e] -= y[2 * e + 1];
+          }
+        }
       }
 #pragma unroll
-      for (int w = 0; w < PARTS; ++w) {
+      for (int d = 0; d < PARTS; ++d) {
         u32 o[6];
 #pragma unroll
-        for (int v = 0; v < 2; ++v) {      // 16 codes of 6 bits in three words
-          const u32* c6 = code[w] + 16 * v;
-          o[3 * v] = c6[0] | c6[1] << 6 | c6[2] << 12 | c6[3] << 18 | c6[4] << 24 | c6[5] << 30;
-          o[3 * v + 1] = c6[5] >> 2 | c6[6] << 4 | c6[7] << 10 | c6[8] << 16 | c6[9] << 22 | c6[10] << 28;
-          o[3 * v + 2] = c6[10] >> 4 | c6[11] << 2 | c6[12] << 8 | c6[13] << 14 | c6[14] << 20 | c6[15] << 26;
-        }
-        op[k][w] = (v8i){(int)o[0], (int)o[1], (int)o[2], (int)o[3], (int)o[4], (int)o[5], 0, 0};
+        for (int i = 0; i < 6; ++i)
+          o[i] = DT != 64 ? w[d][i] : d == 1 ? (g < 2 ? w[2][i] : 0u) : g < 2 ? w[0][i] : Q4 ? 0u : w[1][i];
+        op[k][d] = (v8i){(int)o[0], (int)o[1], (int)o[2], (int)o[3], (int)o[4], (int)o[5], 0, 0};
       }
     }
   }
