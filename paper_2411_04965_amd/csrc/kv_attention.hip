@@ -887,9 +887,9 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attention_wide_kernel(KaArgs
 // then they become probabilities tile by tile, and page q + 1's scores take the registers of a tile as it is used up.  What turn q's
 // products read is bundle q, the values of page q - 1 and the keys of page q + 1, in buffer q % 2; bundle q + 1 is widened into the
 // other buffer meanwhile, from codes that each wave fetched a turn ago.  One barrier a turn.  2048 rows x 32 heads of 128 on 6144 cached:
-// 254 us where calls follow each other (950 TFLOP/s of two products that would be bfloat16's), 290 with both products of a page behind
-// one another and four waves; 8800 clocks a page of 256 rows, of which the matrix unit is busy 3700 and the vector unit about 6000, and
-// the clock falls from 2.4 to 1.9 GHz: the vector unit's softmax and the power bound it.
+// 248 us where calls follow each other (970 TFLOP/s of two products that would be bfloat16's), 290 with both products of a page behind
+// one another and four waves; by the counters 9100 clocks a page of 256 rows, of which a matrix unit is busy 3650 and a vector unit issues
+// for 6400, at 2.1 GHz: the vector unit's softmax bounds it.
 // Probabilities times the values' scales are bfloat16 here: the values widen to bfloat16 once for 8 x QT x 16 rows (levels / 2, the
 // first token's with its lowest bit, exact), and two conversions of the E4M3 pair that few rows take are saved for every score.
 #define KR_WAVES 8
@@ -1398,9 +1398,9 @@ struct KaPlan {
 static KaPlan ka_plan(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t D, int64_t max_pages) {
   // Whole rows where their workgroups (of 128, or 64, rows) are filled and fill the chip's turns: sequences taken to be alike, the share of
   // the row places of all turns that have a row.  A place of the whole rows does about 1.6 times the work of one of the split ones (128
-  // channels; of more, 2.5).  Split / whole, 8 heads of 128: 1 sequence of 256 x 4 rows on 2000 cached (0.25 of the places) 30 / 54 us,
-  // of 400 x 4 on 4000 (0.39) 75 / 92, of 512 x 4 (0.5) 77 / 95; 8 of 200 on 900, 16 heads of 64 (0.78) 58 / 37; 1000 on none, 32 heads
-  // of 64 (0.98) 55 / 32; 16 heads of 256, 2 of 300 on 1000 (0.59) 76 / 54.
+  // channels; of more, 2.5).  Split / whole, 8 heads of 128: 1 sequence of 256 x 4 rows on 2000 cached (0.25 of the places) 25 / 53 us,
+  // of 400 x 4 on 4000 (0.39) 68 / 90, of 512 x 4 (0.5) 69 / 93; 8 of 200 on 900, 16 heads of 64 (0.78) 53 / 36; 1000 on none, 32 heads
+  // of 64 (0.98) 51 / 30; 16 heads of 256, 2 of 300 on 1000 (0.59) 73 / 52.
   const int unit = D > 128 ? 64 : 128;
   const int64_t rows = (T * G + n_seqs - 1) / n_seqs, blocks = (rows + unit - 1) / unit * n_seqs * H, turns = (blocks + 255) / 256;
   if ((double)T * G * H >= (D > 128 ? 0.4 : 0.6) * 256.0 * turns * unit) return {0, 0};
@@ -1413,7 +1413,7 @@ static KaPlan ka_plan(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t D
 
 // Whole rows, up to 128 channels: eight waves of 32 rows (8), whose turn of the chip takes 1.7 times that of eight waves of 16 (7).  Not
 // for a single turn where the new rows are most of their sequences and so see very unlike numbers of pages.  With 16 and 32: 4 sequences
-// of 256 x 4 rows on 2000 cached, 8 heads of 128: 59 and 88 us; 2048 x 4 on 6144, 281 and 254; 4096 on none, 16 heads, 109 and 144.
+// of 256 x 4 rows on 2000 cached, 8 heads of 128: 58 and 84 us; 2048 x 4 on 6144, 279 and 249; 4096 on none, 16 heads, 108 and 139.
 static int ka_rows_shift(int64_t T, int64_t n_seqs, int64_t G, int64_t H, int64_t max_pages) {
   const int64_t rows = (T * G + n_seqs - 1) / n_seqs;
   auto turns = [&](int64_t unit) { return ((rows + unit - 1) / unit * n_seqs * H + 255) / 256; };

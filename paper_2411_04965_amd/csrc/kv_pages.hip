@@ -1,8 +1,8 @@
 // The paged form of the low-bit key / value cache (Section 4.2, Table 3): a batch's new keys and values are rotated (keys),
 // quantized per head to 3 bits, or 4 at position 0, and put into their places; and the way back.
 //   gamma = max |x| over the head,  q = RoundClip(x * (Q_b / (gamma + eps)), -Q_b, Q_b),  scale = gamma / Q_b
-// 2 D bytes of a bfloat16 head in, 3 D / 8 + 4 out: HBM's to bound for prompts (4096 tokens x 32 heads of 128, keys and values: 32 us,
-// 2.9 TB/s; the vector unit takes about as long; 44 with the codes put together bit by bit), the chain of table, row and words for
+// 2 D bytes of a bfloat16 head in, 3 D / 8 + 4 out: HBM's to bound for prompts (4096 tokens x 32 heads of 128, keys and values: 31 us,
+// 2.9 TB/s; the vector units issue for two thirds of the time that CUs hold work; 44 with the codes put together bit by bit), the chain of table, row and words for
 // single tokens (32 sequences x 8 heads: 6.4 us).
 //
 // Workgroup = one head of one page.  Key codes are a token's own 12 byte groups.  Value codes of 32 tokens share words, so the
@@ -299,8 +299,8 @@ int bl_launch_kv_append(const void* K, int64_t ldk, const void* V, int64_t ldv, 
 }
 
 // ---------------------------------------------------------------- reading the codes back
-// value = level * scale, one float32 multiply (bfloat16 outputs: one rounding more).  HBM bound (4096 tokens x 32 heads of 128: 26 us,
-// 3.6 TB/s): a wave stores whole lines of keys, rows of 256 bytes of values.
+// value = level * scale, one float32 multiply (bfloat16 outputs: one rounding more).  4096 tokens x 32 heads of 128: 26 us, 3.6 TB/s,
+// beside vector units that issue for two thirds of the time; a wave stores whole lines of keys, rows of 256 bytes of values.
 __device__ __forceinline__ float kp_level(u32 mag, u32 neg, u32 low, bool four) {
   const float m = (float)(four ? 2 * mag + low : mag);
   return neg ? -m : m;

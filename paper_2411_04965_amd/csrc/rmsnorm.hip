@@ -248,8 +248,9 @@ int bl_launch_rmsnorm_quantize(const void* X, const void* R, bl_dtype dt, int64_
 
 // ---------------------------------------------------------------- gradient
 // With xh = h * rstd, a = dY * gamma:  dX = dH + rstd (a - xh mean(a xh)),  dgamma = sum over tokens of dY * xh.
-// HBM bound: 8 bytes a bfloat16 channel (6 without dH); 4096 x 3200: 28.5 us = 3.7 TB/s.  A workgroup walks over its share of the tokens and keeps its sums of
-// dgamma in registers; the partial sums are added in a fixed order by the second kernel.
+// HBM's to bound: 8 bytes a bfloat16 channel (6 without dH); 4096 x 3200: 28 us = 3.7 TB/s, waves waiting for three quarters of their time
+// (a token's loads start behind the sum of the one before).  A workgroup walks over its share of the tokens and keeps its sums of dgamma in
+// registers; the partial sums are added in a fixed order by the second kernel.
 #define RN_GROUPS 512
 
 template <typename T, int NT, int NV>
