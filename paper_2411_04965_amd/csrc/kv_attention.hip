@@ -1436,7 +1436,8 @@ int bl_launch_kv_attention(const void* Q, int64_t ldq, bl_dtype qdt, int Hq, int
   p.b = b; p.rope = rope;
   p.cs = scale * 1.44269504f;
   p.eps = eps;
-  p.window = window > 0x7FFFFFFF ? 0 : window;      // (no position is that far behind another: every one in reach, and differences fit 64 bits)
+  // (no position is that far behind another: all are in reach, and differences fit 64 bits)
+  p.window = window > 0x7FFFFFFF ? 0 : window;
   p.sinks = (int)(sinks < 0x7FFFFF00 ? sinks : 0x7FFFFF00);
   p.pages = (const unsigned char*)pages;
   p.O = (uint16_t*)O; p.part = (float*)ws;

@@ -2,8 +2,8 @@
 // quantized per head to 3 bits, or 4 at position 0, and put into their places; and the way back.
 //   gamma = max |x| over the head,  q = RoundClip(x * (Q_b / (gamma + eps)), -Q_b, Q_b),  scale = gamma / Q_b
 // 2 D bytes of a bfloat16 head in, 3 D / 8 + 4 out: HBM's to bound for prompts (4096 tokens x 32 heads of 128, keys and values: 31 us,
-// 2.9 TB/s; the vector units issue for two thirds of the time that CUs hold work; 44 with the codes put together bit by bit), the chain of table, row and words for
-// single tokens (32 sequences x 8 heads: 6.4 us).
+// 2.9 TB/s, beside vector units that issue for two thirds of the time that CUs hold work; 44 with the codes put together bit by bit),
+// the chain of table, row and words for single tokens (32 sequences x 8 heads: 6.2 us).
 //
 // Workgroup = one head of one page.  Key codes are a token's own 12 byte groups.  Value codes of 32 tokens share words, so the
 // page's new tokens are coded into LDS first and the words are then put together by one thread each, the bits of older tokens
@@ -46,7 +46,8 @@ __device__ __forceinline__ void kp_load8(const RawT* x, int c, int D, float (&v)
   }
 }
 
-// LPT lanes a token, 8 channels a lane.  A NaN is larger than any number, as where quantize_heads takes its maximum: it has to reach the scale.
+// LPT lanes a token, 8 channels a lane.  A NaN is larger than any number, as where quantize_heads takes its maximum: it has to reach the
+// scale.
 template <int LPT>
 __device__ __forceinline__ float kp_head_max(const float (&v)[8]) {
   float f = 0.0f;
